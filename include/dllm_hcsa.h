@@ -15,7 +15,10 @@
  *   dllm_dense_refresh_attend  dense bidirectional attention, all queries against all keys
  *                              (Refresh phase, Section 2.3 Eq. 3);
  *   dllm_hcsa_pack             gather-copy of each head's kept rows into a dense per-request buffer
- *                              (Section 4.5, the packing done at Refresh time).
+ *                              (Section 4.5, the packing done at Refresh time);
+ *   dllm_hcsa_cache_write, dllm_hcsa_cache_read, dllm_hcsa_select_cached, dllm_hcsa_attend_cached
+ *                              the Reuse phase on a KV cache held in 8 bits per element: rows are quantised as they are
+ *                              written, read back, scored and attended over (see dllm_cache).
  *
  * K and V stay in their dense layout; kept rows are fetched through the index lists at attention time.
  *
@@ -257,6 +260,93 @@ dllm_status dllm_dense_refresh_attend(const dllm_batch *batch,
                                       void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * A KV cache held in 8 bits.
+ *
+ * K and V of a batch's sequences as e4m3 codes (OCP FP8: sign, 4 exponent bits with bias 7, 3 fraction bits; largest 448;
+ * 0x7f and 0xff are NaN; no infinities), in the layout of k and v above with one byte per element.  Every block of
+ * scale_block consecutive tokens of a sequence, counted from its first, has one scale per KV head, K and V apart: a byte c
+ * that stands for 2^(c-127).  An element's value is code * 2^(c-127); it is exact in bf16.  Byte 0 stands for a block of zeros.
+ * Sequence b's i-th block has its scale at k_scale[g * scale_stride_head + cu_kv[b] / scale_block + b + i]: a head's row of
+ * scales has dllm_hcsa_cache_scale_slots(total_kv, batch, scale_block) entries, some of which are not used.
+ *
+ * A write chooses the smallest scale that the block's largest magnitude over 448 allows, between 2^-95 and 2^119, and rounds
+ * value / scale to the nearest code, ties to even: finite values of magnitude up to 448 * 2^119 are off by at most 2^-4 of
+ * themselves or 2^-10 of the scale, whichever is more; larger ones are stored as 448 * 2^119, infinities and NaN as NaN (they
+ * do not count for the scale).
+ * Memory of a new cache must be zero where a part of a block may be written before the rest of it.
+ */
+typedef struct {
+  uint8_t *k, *v;                  /* device, 16-byte aligned; codes of [total_kv, n_kv_heads, head_dim] */
+  uint8_t *k_scale, *v_scale;      /* device; scale bytes [n_kv_heads, scale slots] */
+  int64_t stride_tok, stride_head; /* bytes, multiples of 16, shared by k and v; head_dim stride is 1 */
+  int64_t scale_stride_head;       /* bytes between the rows of scales of two heads */
+  int32_t scale_block;             /* tokens per scale: 16, 32 or 64 */
+} dllm_cache;
+/* Entries of one head's row of scales; -1 for arguments that no cache has (total_kv < 0, batch < 1, another scale_block). */
+int64_t dllm_hcsa_cache_scale_slots(int32_t total_kv, int32_t batch, int32_t scale_block);
+
+/*
+ * Write rows into the cache, quantising them.
+ *
+ * batch describes the cache's sequences (batch, n_kv_heads, head_dim, cu_kv, total_kv, max_kv) and the rows to be written: k and
+ * v with kv_stride_*, of type dtype (bf16 or fp32), [total_rows, n_kv_heads, head_dim].  Its q, cu_q, total_q, max_q, q_stride_* and
+ * softmax_scale are not read.  Rows cu_rows[b] .. cu_rows[b+1]-1 go to positions at[b] .. of sequence b; with at == NULL to its last positions;
+ * with cu_rows == NULL every sequence is written whole (total_rows must be total_kv; max_rows and at are not read).  max_rows
+ * bounds the rows of a sequence.  Rows that would lie outside their sequence are left out.
+ * A block of which rows stay as they were (rows of the sequence that this call does not write) keeps at least its scale; where the
+ * new rows need a larger one, the rows that stay move to it (exactly, but for values below 2^-6 of the new scale, which are
+ * rounded again).  Writing the same rows again changes nothing.
+ * Needs no workspace.  Calls that write into one block at the same time (different streams) race.
+ */
+dllm_status dllm_hcsa_cache_write(const dllm_batch *batch, const dllm_cache *cache,
+                                  const int32_t *cu_rows, /* device, [batch+1], or NULL */
+                                  int32_t total_rows, int32_t max_rows,
+                                  const int32_t *at,      /* device, [batch], or NULL */
+                                  void *hip_stream);
+/*
+ * Read rows back: the same ranges in the other direction, values code * scale in dtype (exact in bf16 and in fp32).  k_out and v_out take the
+ * place of batch->k and batch->v (not read) and have their strides.  Rows outside their sequence are left as they were.
+ */
+dllm_status dllm_hcsa_cache_read(const dllm_batch *batch, const dllm_cache *cache,
+                                 const int32_t *cu_rows, /* device, [batch+1], or NULL */
+                                 int32_t total_rows, int32_t max_rows,
+                                 const int32_t *at,      /* device, [batch], or NULL */
+                                 void *k_out, void *v_out, /* device, 16-byte aligned */
+                                 void *hip_stream);
+
+/*
+ * Selection over the cache: dllm_hcsa_select_ex with K from the cache.  dtype is that of q and must be DLLM_BF16; k, v and
+ * kv_stride_* of batch are not read.  The score of a position is 2^(c-127) times the fma chain over the codes,
+ *     s[j] = 2^(c-127) * (fma chain over d = 0..D-1 of qsum[d] * code[j, h/G, d]),
+ * which is bit for bit the score of the values read back, unless a step of one of the two leaves the range of normal fp32 numbers.
+ * Limits, options, forms (dllm_hcsa_set_select_form) and workspace as for dllm_hcsa_select_ex.
+ */
+size_t dllm_hcsa_select_cached_workspace(const dllm_batch *batch, const dllm_cache *cache, int32_t max_k);
+dllm_status dllm_hcsa_select_cached(const dllm_batch *batch, const dllm_cache *cache,
+                                    const int32_t *cu_k, /* device, [batch+1] */
+                                    int32_t total_k, int32_t max_k, int32_t pool_w,
+                                    int32_t forced_tail, int32_t head_sum,
+                                    int32_t *idx_out,    /* device, [n_q_heads, total_k] */
+                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Attention over the cache: dllm_hcsa_attend without densely attended sequences, K and V from the cache.  dtype is that of q and
+ * o and must be DLLM_BF16; k, v and kv_stride_* of batch are not read.  With idx every head attends over its own list; with idx ==
+ * NULL all heads of a sequence attend over its rows 0 .. k_b-1, which are then read once per KV head: for single tokens of an
+ * autoregressive model (cu_kv gives every sequence's room, cu_k how much of it is filled) or a block over everything.  A
+ * sequence with k_b == 0 gets zeros.  A query whose scores are NaN or overflow to plus infinity, or that attends over a NaN,
+ * gets NaN; no other query's output changes.  A row that no query attends over may hold anything.
+ * The workspace query takes idx or no idx alike.
+ */
+size_t dllm_hcsa_attend_cached_workspace(const dllm_batch *batch, const dllm_cache *cache, int32_t max_k);
+dllm_status dllm_hcsa_attend_cached(const dllm_batch *batch, const dllm_cache *cache,
+                                    const int32_t *idx,  /* device, [n_q_heads, total_k], or NULL */
+                                    const int32_t *cu_k, /* device, [batch+1] */
+                                    int32_t total_k, int32_t max_k,
+                                    void *o,             /* device, [total_q, n_q_heads, head_dim] */
+                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Device-side precondition checks (debug aid).  In a library built with -DDLLM_CHECK_PRECONDITIONS
  * every entry point above first verifies, on the device, the conditions the release library leaves to
  * the caller, and sets bits in one error word per GPU; when a bit is set, every kernel of the call, and
@@ -266,8 +356,8 @@ dllm_status dllm_dense_refresh_attend(const dllm_batch *batch,
  */
 #define DLLM_CHECK_CU_Q 1u      /* cu_q: not starting at 0, decreasing, a sequence above max_q, or not ending at total_q */
 #define DLLM_CHECK_CU_KV 2u     /* the same for cu_kv, max_kv, total_kv */
-#define DLLM_CHECK_CU_K 4u      /* the same for cu_k, max_k, total_k */
-#define DLLM_CHECK_K_OVER_L 8u  /* a sparse sequence keeps more rows than it has */
+#define DLLM_CHECK_CU_K 4u      /* the same for cu_k, max_k, total_k (cache calls: cu_rows, max_rows, total_rows) */
+#define DLLM_CHECK_K_OVER_L 8u  /* a sparse sequence keeps (cache calls: moves) more rows than it has */
 #define DLLM_CHECK_FORCED 16u   /* a sequence with kept rows keeps, or has, fewer than forced_tail rows */
 #define DLLM_CHECK_IDX 32u      /* an index outside [0, L_b) in a sparse sequence's list */
 dllm_status dllm_hcsa_precondition_errors(void *hip_stream, uint32_t *errors_out /* host */);

@@ -20,7 +20,7 @@ BUILD_DIR = os.path.join(_HERE, "_build")
 LIB_PATH = os.path.join(_HERE, "libdllm_hcsa.so")
 
 SOURCES = ["api.hip", "checks.hip", "select_kernels.hip", "pack_kernels.hip", "attend_f32.hip",
-           "attend_sparse_bf16.hip", "attend_dense_bf16.hip", "attend_dense_paired_bf16.hip"]
+           "attend_sparse_bf16.hip", "attend_dense_bf16.hip", "attend_dense_paired_bf16.hip", "cache_kernels.hip", "attend_cache.hip"]
 # the same sources with the device-side precondition checks compiled in (a debugging aid, see include/dllm_hcsa.h)
 LIB_PATH_CHECKED = os.path.join(_HERE, "libdllm_hcsa_checked.so")
 CHECKED_FLAGS = ["-DDLLM_CHECK_PRECONDITIONS"]
@@ -34,7 +34,8 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "
 # selection in the median of 500 short calls, 0.4 on the mixed fp32 step (29.6 -> 29.2); longer ones gain no more than two runs
 # differ by.  Not the dense kernels, whose start waits for the batch's offsets anyway (one layer 22.04 / 22.12 us).
 PRELOAD_FLAGS = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
-PRELOAD_SOURCES = {"select_kernels.hip", "attend_f32.hip", "attend_sparse_bf16.hip", "pack_kernels.hip"}
+PRELOAD_SOURCES = {"select_kernels.hip", "attend_f32.hip", "attend_sparse_bf16.hip", "pack_kernels.hip", "cache_kernels.hip",
+                   "attend_cache.hip"}
 
 
 def _hipcc() -> str:

@@ -28,8 +28,12 @@ dllm_status fail(dllm_status st, const char* fmt, ...) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// What of the descriptor a call reads beside the sizes: the queries, the dense K and V.
+enum : unsigned { kReadsQ = 1, kReadsKV = 2 };
+
 // Validates the batch descriptor and fills the kernel-side shape.
-dllm_status check_batch(const dllm_batch* b, dllm::Shape* out) {
+dllm_status check_batch(const dllm_batch* b, dllm::Shape* out, unsigned reads = kReadsQ | kReadsKV) {
+  const bool with_q = reads & kReadsQ, with_kv = reads & kReadsKV;
   if (b == nullptr) return fail(DLLM_ERR_INVALID_ARG, "batch descriptor is NULL");
   if (b->dtype != DLLM_F32 && b->dtype != DLLM_BF16)
     return fail(DLLM_ERR_INVALID_ARG, "dtype %d is neither DLLM_F32 nor DLLM_BF16", int(b->dtype));
@@ -40,37 +44,104 @@ dllm_status check_batch(const dllm_batch* b, dllm::Shape* out) {
     return fail(DLLM_ERR_INVALID_ARG, "n_q_heads %d is not a multiple of n_kv_heads %d", b->n_q_heads, b->n_kv_heads);
   if (b->head_dim != 64 && b->head_dim != 128)
     return fail(DLLM_ERR_INVALID_ARG, "head_dim %d is not 64 or 128", b->head_dim);
-  if (!b->q || !b->k || !b->v) return fail(DLLM_ERR_INVALID_ARG, "q, k and v must be non-NULL");
-  if (!b->cu_q || !b->cu_kv) return fail(DLLM_ERR_INVALID_ARG, "cu_q and cu_kv must be non-NULL");
-  if (b->total_q < 0 || b->total_kv < 0 || b->max_q < 0 || b->max_kv < 0 || b->max_q > b->total_q ||
+  if ((with_q && !b->q) || (with_kv && (!b->k || !b->v)))
+    return fail(DLLM_ERR_INVALID_ARG, with_q && with_kv ? "q, k and v must be non-NULL"
+                                      : with_q          ? "q must be non-NULL"
+                                                        : "k and v must be non-NULL");
+  if ((with_q && !b->cu_q) || !b->cu_kv)
+    return fail(DLLM_ERR_INVALID_ARG, with_q ? "cu_q and cu_kv must be non-NULL" : "cu_kv must be non-NULL");
+  if ((with_q && (b->total_q < 0 || b->max_q < 0 || b->max_q > b->total_q)) || b->total_kv < 0 || b->max_kv < 0 ||
       b->max_kv > b->total_kv)
     return fail(DLLM_ERR_INVALID_ARG, "need 0 <= max_q <= total_q and 0 <= max_kv <= total_kv (got %d/%d, %d/%d)",
                 b->max_q, b->total_q, b->max_kv, b->total_kv);
   const int es = b->dtype == DLLM_F32 ? 4 : 2;
   const int64_t per16 = 16 / es;
-  if (b->q_stride_head < b->head_dim || b->kv_stride_head < b->head_dim || b->q_stride_tok < b->head_dim ||
-      b->kv_stride_tok < b->head_dim)
+  if ((with_q && (b->q_stride_head < b->head_dim || b->q_stride_tok < b->head_dim)) ||
+      (with_kv && (b->kv_stride_head < b->head_dim || b->kv_stride_tok < b->head_dim)))
     return fail(DLLM_ERR_INVALID_ARG, "strides must be at least head_dim elements");
-  if (b->q_stride_tok % per16 || b->q_stride_head % per16 || b->kv_stride_tok % per16 || b->kv_stride_head % per16)
+  if ((with_q && (b->q_stride_tok % per16 || b->q_stride_head % per16)) ||
+      (with_kv && (b->kv_stride_tok % per16 || b->kv_stride_head % per16)))
     return fail(DLLM_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
-  if (!aligned16(b->q) || !aligned16(b->k) || !aligned16(b->v))
+  if ((with_q && !aligned16(b->q)) || (with_kv && (!aligned16(b->k) || !aligned16(b->v))))
     return fail(DLLM_ERR_INVALID_ARG, "q, k and v must be 16-byte aligned");
-  if (!std::isfinite(b->softmax_scale) || !(b->softmax_scale > 0.0f))
+  if (with_q && (!std::isfinite(b->softmax_scale) || !(b->softmax_scale > 0.0f)))
     return fail(DLLM_ERR_INVALID_ARG, "softmax_scale must be finite and positive");
   out->batch = b->batch;
   out->hq = b->n_q_heads;
   out->hkv = b->n_kv_heads;
   out->group = b->n_q_heads / b->n_kv_heads;
   out->d = b->head_dim;
-  out->q_tok = b->q_stride_tok;
-  out->q_head = b->q_stride_head;
-  out->kv_tok = b->kv_stride_tok;
-  out->kv_head = b->kv_stride_head;
-  out->total_q = b->total_q;
+  out->q_tok = with_q ? b->q_stride_tok : 0;
+  out->q_head = with_q ? b->q_stride_head : 0;
+  out->kv_tok = with_kv ? b->kv_stride_tok : 0;
+  out->kv_head = with_kv ? b->kv_stride_head : 0;
+  out->total_q = with_q ? b->total_q : 0;
   out->total_kv = b->total_kv;
-  out->max_q = b->max_q;
+  out->max_q = with_q ? b->max_q : 0;
   out->max_kv = b->max_kv;
-  out->scale = b->softmax_scale;
+  out->scale = with_q ? b->softmax_scale : 0.0f;
+  return DLLM_OK;
+}
+
+int shift_of(int32_t scale_block) { return scale_block == 16 ? 4 : scale_block == 32 ? 5 : scale_block == 64 ? 6 : -1; }
+
+// Validates the cache descriptor against the batch (whose own checks have passed) and fills the kernels' view of it.
+dllm_status check_cache(const dllm_cache* c, const dllm_batch* b, dllm::CacheView* out) {
+  if (c == nullptr) return fail(DLLM_ERR_INVALID_ARG, "cache descriptor is NULL");
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale)
+    return fail(DLLM_ERR_INVALID_ARG, "the cache's k, v, k_scale and v_scale must be non-NULL");
+  if (shift_of(c->scale_block) < 0) return fail(DLLM_ERR_INVALID_ARG, "scale_block %d is not 16, 32 or 64", c->scale_block);
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(DLLM_ERR_INVALID_ARG, "the cache's k and v must be 16-byte aligned");
+  if (c->stride_tok < b->head_dim || c->stride_head < b->head_dim)
+    return fail(DLLM_ERR_INVALID_ARG, "the cache's strides must be at least head_dim bytes");
+  if (c->stride_tok % 16 || c->stride_head % 16)
+    return fail(DLLM_ERR_INVALID_ARG, "the cache's strides must be multiples of 16 bytes");
+  if (b->total_kv > INT32_MAX - 128) return fail(DLLM_ERR_UNSUPPORTED, "total_kv %d is within 128 of 2^31", b->total_kv);
+  const int64_t slots = dllm_hcsa_cache_scale_slots(b->total_kv, b->batch, c->scale_block);
+  if (c->scale_stride_head < slots)
+    return fail(DLLM_ERR_INVALID_ARG, "scale_stride_head %lld is less than the %lld scales of a head",
+                static_cast<long long>(c->scale_stride_head), static_cast<long long>(slots));
+  out->k = c->k;
+  out->v = c->v;
+  out->ks = c->k_scale;
+  out->vs = c->v_scale;
+  out->tok = c->stride_tok;
+  out->head = c->stride_head;
+  out->scale_head = c->scale_stride_head;
+  out->shift = shift_of(c->scale_block);
+  return DLLM_OK;
+}
+
+// Both descriptors of a call that reads queries and the cache.
+dllm_status check_cached_call(const dllm_batch* b, const dllm_cache* c, dllm::Shape* s, dllm::CacheView* view) {
+  dllm_status st = check_batch(b, s, kReadsQ);
+  if (st != DLLM_OK) return st;
+  if ((st = check_cache(c, b, view)) != DLLM_OK) return st;
+  if (b->dtype != DLLM_BF16)
+    return fail(DLLM_ERR_UNSUPPORTED, "queries beside an 8-bit cache must be bf16 (dtype %d)", int(b->dtype));
+  s->kv_tok = view->tok;   // in bytes, as a code is one
+  s->kv_head = view->head;
+  return DLLM_OK;
+}
+
+// Ranges of rows that dllm_hcsa_cache_write and _read move.
+dllm_status check_rows(const dllm_batch* b, const dllm::Shape& s, const dllm::CacheView& c, const int32_t* cu_rows,
+                       int32_t total_rows, int32_t max_rows, const int32_t* at, dllm::RowRange* out) {
+  if (cu_rows == nullptr) {
+    if (total_rows != b->total_kv)
+      return fail(DLLM_ERR_INVALID_ARG, "without cu_rows all rows are moved: total_rows must be total_kv (got %d, %d)", total_rows,
+                  b->total_kv);
+    *out = {nullptr, nullptr, b->max_kv};
+  } else {
+    if (total_rows < 0 || max_rows < 0 || max_rows > total_rows || max_rows > b->max_kv)
+      return fail(DLLM_ERR_INVALID_ARG, "need 0 <= max_rows <= min(total_rows, max_kv) (got max_rows=%d, total_rows=%d, max_kv=%d)",
+                  max_rows, total_rows, b->max_kv);
+    *out = {cu_rows, at, max_rows};
+  }
+  const int64_t blocks = (int64_t(out->max_rows) >> c.shift) + 2, groups = (2 * int64_t(s.hkv) + 3) / 4;
+  if (blocks * groups >= (int64_t(1) << 24))
+    return fail(DLLM_ERR_UNSUPPORTED, "%lld blocks of %d KV heads in one sequence are more than one call takes",
+                static_cast<long long>(blocks), s.hkv);
   return DLLM_OK;
 }
 
@@ -122,13 +193,11 @@ dllm_status check_select_scalars(const dllm_batch* b, int32_t max_k, int32_t poo
 }
 
 
-// Scalar and pointer checks shared by the selection entry points; fills the kernel-side shape.
-dllm_status check_select_call(const dllm_batch* batch, const int32_t* cu_k, int32_t total_k, int32_t max_k,
-                              int32_t pool_w, int32_t forced_tail, int32_t head_sum, const int32_t* idx_out,
-                              dllm::Shape* s) {
-  dllm_status st = check_batch(batch, s);
+// Scalar and pointer checks shared by the selection entry points.
+dllm_status check_select_arguments(const dllm_batch* batch, const int32_t* cu_k, int32_t total_k, int32_t max_k, int32_t pool_w,
+                                   int32_t forced_tail, int32_t head_sum, const int32_t* idx_out) {
+  const dllm_status st = check_select_scalars(batch, max_k, pool_w);
   if (st != DLLM_OK) return st;
-  if ((st = check_select_scalars(batch, max_k, pool_w)) != DLLM_OK) return st;
   if (cu_k == nullptr || idx_out == nullptr) return fail(DLLM_ERR_INVALID_ARG, "cu_k and idx_out must be non-NULL");
   if (total_k < 1 || max_k > total_k)
     return fail(DLLM_ERR_INVALID_ARG, "need 1 <= max_k <= total_k (got max_k=%d, total_k=%d)", max_k, total_k);
@@ -136,6 +205,15 @@ dllm_status check_select_call(const dllm_batch* batch, const int32_t* cu_k, int3
     return fail(DLLM_ERR_INVALID_ARG, "forced_tail %d outside 0..max_k (%d)", forced_tail, max_k);
   if (head_sum != 0 && head_sum != 1) return fail(DLLM_ERR_INVALID_ARG, "head_sum must be 0 or 1 (got %d)", head_sum);
   return DLLM_OK;
+}
+
+// ... with those of a batch of dense K; fills the kernel-side shape.
+dllm_status check_select_call(const dllm_batch* batch, const int32_t* cu_k, int32_t total_k, int32_t max_k,
+                              int32_t pool_w, int32_t forced_tail, int32_t head_sum, const int32_t* idx_out,
+                              dllm::Shape* s) {
+  dllm_status st = check_batch(batch, s);
+  if (st != DLLM_OK) return st;
+  return check_select_arguments(batch, cu_k, total_k, max_k, pool_w, forced_tail, head_sum, idx_out);
 }
 
 constexpr int kMaxDevices = 64;
@@ -246,7 +324,7 @@ extern "C" {
 
 const char* dllm_last_error(void) { return g_err; }
 
-int32_t dllm_hcsa_version(void) { return 100; }
+int32_t dllm_hcsa_version(void) { return 200; }
 
 size_t dllm_hcsa_select_workspace(const dllm_batch* batch, int32_t max_k) {
   dllm::Shape s;
@@ -277,7 +355,7 @@ int32_t dllm_hcsa_set_select_form(int32_t form) { return dllm::set_select_form(f
 int32_t dllm_hcsa_select_form_of(const dllm_batch* batch, int32_t pool_w, int32_t head_sum) {
   dllm::Shape s;
   if (check_batch(batch, &s) != DLLM_OK) return -1;
-  return dllm::select_form_of(s, batch->dtype, pool_w, head_sum);
+  return dllm::select_form_of(s, batch->dtype == DLLM_BF16 ? 2 : 4, pool_w, head_sum);
 }
 
 dllm_status dllm_hcsa_select_static(const dllm_batch* batch, const int32_t* cu_k, int32_t total_k, int32_t max_k,
@@ -394,6 +472,112 @@ dllm_status dllm_hcsa_pack(const dllm_batch* batch, const int32_t* idx, const in
     e = dllm::launch_pack(s, batch->dtype, batch->k, batch->v, batch->cu_kv, idx, cu_k, total_k, max_k, k_packed,
                           v_packed, stream);
   return device_result(e, "dllm_hcsa_pack");
+}
+
+int64_t dllm_hcsa_cache_scale_slots(int32_t total_kv, int32_t batch, int32_t scale_block) {
+  const int shift = shift_of(scale_block);
+  return shift < 0 || total_kv < 0 || batch < 1 ? -1 : (int64_t(total_kv) >> shift) + batch;
+}
+
+dllm_status dllm_hcsa_cache_write(const dllm_batch* batch, const dllm_cache* cache, const int32_t* cu_rows, int32_t total_rows,
+                                  int32_t max_rows, const int32_t* at, void* hip_stream) {
+  dllm::Shape s;
+  dllm::CacheView view;
+  dllm::RowRange rows;
+  dllm_status st = check_batch(batch, &s, kReadsKV);
+  if (st != DLLM_OK) return st;
+  if ((st = check_cache(cache, batch, &view)) != DLLM_OK) return st;
+  if ((st = check_rows(batch, s, view, cu_rows, total_rows, max_rows, at, &rows)) != DLLM_OK) return st;
+  g_err[0] = 0;
+  if (rows.max_rows == 0) return DLLM_OK;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  s.total_q = s.total_kv;   // (the validators walk cu_kv in the place of cu_q)
+  s.max_q = s.max_kv;
+  hipError_t e = dllm::validate_inputs(s, batch->cu_kv, batch->cu_kv, cu_rows, nullptr, nullptr, total_rows, max_rows, 0, stream);
+  if (e == hipSuccess) e = dllm::launch_cache_write(s, batch->dtype, view, rows, batch->k, batch->v, batch->cu_kv, stream);
+  return device_result(e, "dllm_hcsa_cache_write");
+}
+
+dllm_status dllm_hcsa_cache_read(const dllm_batch* batch, const dllm_cache* cache, const int32_t* cu_rows, int32_t total_rows,
+                                 int32_t max_rows, const int32_t* at, void* k_out, void* v_out, void* hip_stream) {
+  dllm::Shape s;
+  dllm::CacheView view;
+  dllm::RowRange rows;
+  if (batch == nullptr) return fail(DLLM_ERR_INVALID_ARG, "batch descriptor is NULL");
+  dllm_batch out = *batch;
+  out.k = k_out;
+  out.v = v_out;
+  dllm_status st = check_batch(&out, &s, kReadsKV);
+  if (st != DLLM_OK) return st;
+  if ((st = check_cache(cache, batch, &view)) != DLLM_OK) return st;
+  if ((st = check_rows(batch, s, view, cu_rows, total_rows, max_rows, at, &rows)) != DLLM_OK) return st;
+  g_err[0] = 0;
+  if (rows.max_rows == 0) return DLLM_OK;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  s.total_q = s.total_kv;
+  s.max_q = s.max_kv;
+  hipError_t e = dllm::validate_inputs(s, batch->cu_kv, batch->cu_kv, cu_rows, nullptr, nullptr, total_rows, max_rows, 0, stream);
+  if (e == hipSuccess) e = dllm::launch_cache_read(s, batch->dtype, view, rows, k_out, v_out, batch->cu_kv, stream);
+  return device_result(e, "dllm_hcsa_cache_read");
+}
+
+size_t dllm_hcsa_select_cached_workspace(const dllm_batch* batch, const dllm_cache* cache, int32_t max_k) {
+  dllm::Shape s;
+  dllm::CacheView view;
+  if (check_cached_call(batch, cache, &s, &view) != DLLM_OK) return 0;
+  (void)max_k;
+  return dllm::plan_select(s).bytes;
+}
+
+dllm_status dllm_hcsa_select_cached(const dllm_batch* batch, const dllm_cache* cache, const int32_t* cu_k, int32_t total_k,
+                                    int32_t max_k, int32_t pool_w, int32_t forced_tail, int32_t head_sum, int32_t* idx_out,
+                                    void* workspace, size_t workspace_bytes, void* hip_stream) {
+  dllm::Shape s;
+  dllm::CacheView view;
+  dllm_status st = check_cached_call(batch, cache, &s, &view);
+  if (st != DLLM_OK) return st;
+  if ((st = check_select_arguments(batch, cu_k, total_k, max_k, pool_w, forced_tail, head_sum, idx_out)) != DLLM_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, dllm::plan_select(s).bytes)) != DLLM_OK) return st;
+  g_err[0] = 0;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = dllm::validate_inputs(s, batch->cu_q, batch->cu_kv, cu_k, nullptr, nullptr, total_k, max_k, forced_tail,
+                                       stream);
+  if (e == hipSuccess)
+    e = dllm::launch_select_cached(s, view, batch->q, batch->cu_q, batch->cu_kv, cu_k, total_k, pool_w, forced_tail, head_sum,
+                                   idx_out, workspace, stream);
+  return device_result(e, "dllm_hcsa_select_cached");
+}
+
+size_t dllm_hcsa_attend_cached_workspace(const dllm_batch* batch, const dllm_cache* cache, int32_t max_k) {
+  dllm::Shape s;
+  dllm::CacheView view;
+  if (check_cached_call(batch, cache, &s, &view) != DLLM_OK || max_k < 0) return 0;
+  return dllm::attend_cached_workspace(s, max_k);
+}
+
+dllm_status dllm_hcsa_attend_cached(const dllm_batch* batch, const dllm_cache* cache, const int32_t* idx, const int32_t* cu_k,
+                                    int32_t total_k, int32_t max_k, void* o, void* workspace, size_t workspace_bytes,
+                                    void* hip_stream) {
+  dllm::Shape s;
+  dllm::CacheView view;
+  dllm_status st = check_cached_call(batch, cache, &s, &view);
+  if (st != DLLM_OK) return st;
+  if (o == nullptr || cu_k == nullptr) return fail(DLLM_ERR_INVALID_ARG, "o and cu_k must be non-NULL");
+  if (!aligned16(o)) return fail(DLLM_ERR_INVALID_ARG, "o must be 16-byte aligned");
+  if (total_k < 0 || max_k < 0 || max_k > total_k || max_k > batch->max_kv)
+    return fail(DLLM_ERR_INVALID_ARG, "need 0 <= max_k <= min(total_k, max_kv) (got max_k=%d, total_k=%d, max_kv=%d)",
+                max_k, total_k, batch->max_kv);
+  if (view.tok >= (int64_t(1) << 24) || batch->max_kv > (1 << 24) || int64_t(batch->max_kv) * view.tok >= (int64_t(1) << 32))
+    return fail(DLLM_ERR_UNSUPPORTED,
+                "one sequence must have at most 2^24 rows spanning < 4 GiB with a token stride < 16 MiB (max_kv=%d, stride_tok=%lld)",
+                batch->max_kv, static_cast<long long>(view.tok));
+  if ((st = check_workspace(workspace, workspace_bytes, dllm::attend_cached_workspace(s, max_k))) != DLLM_OK) return st;
+  g_err[0] = 0;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = dllm::validate_inputs(s, batch->cu_q, batch->cu_kv, cu_k, idx, nullptr, total_k, max_k, 0, stream);
+  if (e == hipSuccess)
+    e = dllm::launch_attend_cached(s, view, max_k, batch->q, batch->cu_q, batch->cu_kv, idx, cu_k, total_k, o, workspace, stream);
+  return device_result(e, "dllm_hcsa_attend_cached");
 }
 
 size_t dllm_dense_refresh_attend_workspace(const dllm_batch* batch) {

@@ -39,6 +39,24 @@ inline bool gathers_once(const Shape& s, int es) { return k_bytes(s, es) > (int6
 
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
+// ---- 8-bit cache (cache_kernels.hip): codes and scales of one call, strides in bytes
+struct CacheView {
+  uint8_t *k, *v;          // codes
+  uint8_t *ks, *vs;        // scale bytes, [hkv][scale_head]
+  int64_t tok, head;       // of k and v
+  int64_t scale_head;
+  int32_t shift;           // log2 of the tokens per scale
+};
+// A sequence's rows from `at` on (NULL: its last rows) that a call moves; cu_rows NULL: all rows of every sequence.
+struct RowRange {
+  const int32_t *cu_rows, *at;
+  int32_t max_rows;
+};
+hipError_t launch_cache_write(const Shape& s, dllm_dtype dt, const CacheView& c, const RowRange& r, const void* k, const void* v,
+                              const int32_t* cu_kv, hipStream_t st);
+hipError_t launch_cache_read(const Shape& s, dllm_dtype dt, const CacheView& c, const RowRange& r, void* k, void* v,
+                             const int32_t* cu_kv, hipStream_t st);
+
 // ---- selection (select_kernels.hip)
 struct SelectPlan {
   size_t off_scores, off_summed, bytes;
@@ -49,8 +67,14 @@ hipError_t launch_select(const Shape& s, dllm_dtype dt, const void* q, const voi
                          int32_t pool_w, int32_t forced_tail, int32_t head_sum, int32_t* idx_out, void* ws,
                          hipStream_t st);
 
+// the same over the K of an 8-bit cache (bf16 queries; kv_tok and kv_head of the shape are in bytes)
+hipError_t launch_select_cached(const Shape& s, const CacheView& c, const void* q, const int32_t* cu_q, const int32_t* cu_kv,
+                                const int32_t* cu_k, int32_t total_k, int32_t pool_w, int32_t forced_tail, int32_t head_sum,
+                                int32_t* idx_out, void* ws, hipStream_t st);
+
 // the form a selection call of this shape takes under the current setting (ONE_LAUNCH or TWO_LAUNCHES)
-int32_t select_form_of(const Shape& s, dllm_dtype dt, int32_t pool_w, int32_t head_sum);
+// (es: bytes per element of K)
+int32_t select_form_of(const Shape& s, int es, int32_t pool_w, int32_t head_sum);
 int32_t set_select_form(int32_t form);   // DLLM_SELECT_FORM_*; returns the previous one, -1 if form is not one of them
 
 // ---- packing of the kept rows (pack_kernels.hip)
@@ -81,6 +105,15 @@ hipError_t launch_attend_sparse_bf16(const Shape& s, const AttendPlan& p, const 
                                      const void* v, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* idx,
                                      const int32_t* cu_k, int32_t total_k, const uint8_t* seq_mode, void* o,
                                      void* ws, hipStream_t st);
+// The same over an 8-bit cache; without lists (idx NULL) all heads attend over the first rows of their sequence.
+size_t attend_cached_workspace(const Shape& s, int32_t max_k);   // enough for a call with lists and for one without
+hipError_t launch_attend_cached(const Shape& s, const CacheView& c, int32_t max_k, const void* q, const int32_t* cu_q,
+                                const int32_t* cu_kv, const int32_t* idx, const int32_t* cu_k, int32_t total_k, void* o, void* ws,
+                                hipStream_t st);
+// merges the partial results of lists that were cut into chunks
+hipError_t launch_merge_chunks(const Shape& s, const AttendPlan& p, const int32_t* cu_q, const int32_t* cu_k,
+                               const uint8_t* seq_mode, const float* po, const float* pm, const float* pl, void* o,
+                               hipStream_t st);
 hipError_t launch_attend_dense_bf16(const Shape& s, const void* q, const void* k, const void* v,
                                     const int32_t* cu_q, const int32_t* cu_kv, const uint8_t* seq_mode, int which,
                                     void* o, hipStream_t st);
@@ -148,6 +181,12 @@ __device__ __forceinline__ int rank_longest_first(int length, int batch) {
     for (int c = 0; c < 8; ++c) rank += uint32_t(__builtin_amdgcn_readlane(int(key), i + c)) > key ? 1 : 0;
   return lane < batch ? rank : lane;
 }
+
+// The value 2^(c-127) of a scale byte of the 8-bit cache.  (Byte 0 stands beside zeros only; what it is taken for does not matter.)
+__device__ __forceinline__ float scale_of(uint32_t c) { return __uint_as_float(c << 23); }
+// Where the scales of sequence b begin in a head's row of them: every sequence starts a block of its own, so the floor of
+// its first row plus one slot per sequence before it leaves room for a part block at the end of each.
+__device__ __forceinline__ int scale_slot(int kv0, int b, int shift) { return (kv0 >> shift) + b; }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

@@ -74,18 +74,60 @@ __device__ __forceinline__ float fma_row_bcast(float acc, float vq, const float 
   return acc;
 }
 
+// The numbers in one 16-byte chunk of a K row: bf16, fp32, or e4m3 codes (of the 8-bit cache; their scale is applied to the
+// finished sum).  The products take them eight at a time at most.
+template <int ES>
+__device__ __forceinline__ void widen_chunk(v4u x, float (&kv)[16 / ES]) {
+  if constexpr (ES == 1) {
+    typedef __attribute__((ext_vector_type(2))) float f2;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[e]), false), b = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[e]), true);
+      kv[4 * e] = a.x; kv[4 * e + 1] = a.y; kv[4 * e + 2] = b.x; kv[4 * e + 3] = b.y;
+    }
+  } else if constexpr (ES == 2) {
+    kv[0] = bf16_lo(x.x); kv[1] = bf16_hi(x.x); kv[2] = bf16_lo(x.y); kv[3] = bf16_hi(x.y);
+    kv[4] = bf16_lo(x.z); kv[5] = bf16_hi(x.z); kv[6] = bf16_lo(x.w); kv[7] = bf16_hi(x.w);
+  } else {
+    kv[0] = __uint_as_float(x.x); kv[1] = __uint_as_float(x.y);
+    kv[2] = __uint_as_float(x.z); kv[3] = __uint_as_float(x.w);
+  }
+}
+template <int J, int N>
+__device__ __forceinline__ float fma_chunk(float acc, float vq, const float (&kv)[N]) {
+  if constexpr (N == 16) {
+    float lo[8], hi[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { lo[e] = kv[e]; hi[e] = kv[8 + e]; }
+    return fma_row_bcast<8>(fma_row_bcast<0>(acc, vq, lo), vq, hi);
+  } else {
+    return fma_row_bcast<J>(acc, vq, kv);
+  }
+}
+
+// Scales of a cached K (8-bit cache only): scale bytes per KV head and block of 2^shift tokens.
+struct KeyScales {
+  const uint8_t* at;
+  int64_t head;
+  int32_t shift;
+};
+__device__ __forceinline__ KeyScales scales_of(const KeyScales& x) { return x; }
+
 // f(integral_constant<int, 0>), f(integral_constant<int, 1>), ... in order
 template <typename F, int... C>
 __device__ __forceinline__ void for_each_index(F& f, std::integer_sequence<int, C...>) {
   (f(std::integral_constant<int, C>{}), ...);
 }
 
-template <int ES, int D, int GT, bool Once>
+// Scales: nothing, or KeyScales with ES = 1 (e4m3 codes; the queries are bf16).
+template <int ES, int D, int GT, bool Once, typename... Scales>
 __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void score_kernel(
     const char* __restrict__ k, const char* __restrict__ q, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ cu_kv, const int32_t* __restrict__ cu_k, float* __restrict__ scores,
-    int tiles_per_wave, Shape s DLLM_CHECK_PARAM) {
+    int tiles_per_wave, Shape s, Scales... scales DLLM_CHECK_PARAM) {
   DLLM_CHECK_EXIT();
+  static_assert(sizeof...(Scales) == (ES == 1 ? 1 : 0), "codes have scales");
+  constexpr int QES = ES == 1 ? 2 : ES;   // bytes per element of the queries
   constexpr int ROWB = D * ES;
   constexpr int CH = ROWB / 16;   // 16-byte chunks per row
   constexpr int EPC = 16 / ES;    // elements per chunk
@@ -115,6 +157,13 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   const int sw = swz<CH>(lane);
 
   v4u regs[CH];
+  uint32_t unit = 0;   // scale byte of the row that this lane scores
+  auto fetch_unit = [&](int r0) {
+    if constexpr (ES == 1) {
+      const KeyScales sc = scales_of(scales...);
+      unit = sc.at[g * sc.head + scale_slot(kv0, b, sc.shift) + (min(r0 + lane, L - 1) >> sc.shift)];
+    }
+  };
   // rows past the end of the sequence re-read its last row; their scores are never stored
   auto fetch = [&](int r0) {
 #pragma unroll
@@ -123,7 +172,7 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
       regs[i] = load_once<Once>(base + row * row_pitch);
     }
   };
-  if (ntiles > 0) fetch(first);
+  if (ntiles > 0) { fetch(first); fetch_unit(first); }
 
   // While the first rows are on their way: the block sums of this KV head's query heads,
   // sum[hh][d] = sum over the block's query rows in ascending row order, fp32 (the canonical order).
@@ -131,15 +180,15 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   // and stay in L2), so selection needs no reduction launch of its own.
   {
     const int nq = q1 - q0;
-    const int64_t qpitch = s.q_tok * ES;
+    const int64_t qpitch = s.q_tok * QES;
     auto widen = [](const char* p) -> float {
-      if constexpr (ES == 2)
+      if constexpr (QES == 2)
         return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
       else
         return *reinterpret_cast<const float*>(p);
     };
     for (int e = threadIdx.x; e < s.group * D; e += kScoreWaves * 64) {
-      const char* p = q + (int64_t(q0) * s.q_tok + int64_t(g * s.group + e / D) * s.q_head + e % D) * ES;
+      const char* p = q + (int64_t(q0) * s.q_tok + int64_t(g * s.group + e / D) * s.q_head + e % D) * QES;
       float a = 0.0f;
       int i = 0;
       for (; i + 32 <= nq; i += 32) {   // a whole block of 32 queries: all loads in flight, then the adds in row order
@@ -184,7 +233,8 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
       const int f = i * 64 + lane, row = f / CH, c = f % CH;
       mine[row * CH + (c ^ swz<CH>(row))] = regs[i];
     }
-    if (it + 1 < ntiles) fetch(r0 + 64);
+    const uint32_t unit_now = unit;
+    if (it + 1 < ntiles) { fetch(r0 + 64); fetch_unit(r0 + 64); }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -200,17 +250,15 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
         constexpr int c = decltype(cc)::value;
         const v4u x = mine[lane * CH + (c ^ sw)];
         float kv[EPC];
-        if constexpr (ES == 2) {
-          kv[0] = bf16_lo(x.x); kv[1] = bf16_hi(x.x); kv[2] = bf16_lo(x.y); kv[3] = bf16_hi(x.y);
-          kv[4] = bf16_lo(x.z); kv[5] = bf16_hi(x.z); kv[6] = bf16_lo(x.w); kv[7] = bf16_hi(x.w);
-        } else {
-          kv[0] = __uint_as_float(x.x); kv[1] = __uint_as_float(x.y);
-          kv[2] = __uint_as_float(x.z); kv[3] = __uint_as_float(x.w);
-        }
+        widen_chunk<ES>(x, kv);
 #pragma unroll
-        for (int t = 0; t < GT; ++t) acc[t] = fma_row_bcast<(c * EPC) % 16, EPC>(acc[t], vq[t][(c * EPC) / 16], kv);
+        for (int t = 0; t < GT; ++t) acc[t] = fma_chunk<(c * EPC) % 16, EPC>(acc[t], vq[t][(c * EPC) / 16], kv);
       };
       for_each_index(chunk, std::make_integer_sequence<int, CH>{});
+      if constexpr (ES == 1) {   // a power of two: exact, unless the product leaves the range of normal numbers
+#pragma unroll
+        for (int t = 0; t < GT; ++t) acc[t] = acc[t] * scale_of(unit_now);
+      }
       if (r0 + lane < L) {
 #pragma unroll
         for (int t = 0; t < GT; ++t)
@@ -707,12 +755,14 @@ __device__ __forceinline__ uint3 pick_bin(const uint32_t* hrow, uint32_t kth, in
 // to pick up the previous compare's.
 __device__ __forceinline__ void set_lane(uint32_t& v, uint32_t x, int u) { v = int(threadIdx.x & 63) == u ? x : v; }
 
-template <int ES, int D, int GT, int NT>
+template <int ES, int D, int GT, int NT, typename... Scales>
 __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void select_fused_kernel(
     const char* __restrict__ k, const char* __restrict__ q, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ cu_kv, const int32_t* __restrict__ cu_k, int32_t total_k, int32_t forced_tail,
-    int32_t pool_w, int32_t ranked, int32_t* __restrict__ idx_out, Shape s DLLM_CHECK_PARAM) {
+    int32_t pool_w, int32_t ranked, int32_t* __restrict__ idx_out, Shape s, Scales... scales DLLM_CHECK_PARAM) {
   DLLM_CHECK_EXIT();
+  static_assert(sizeof...(Scales) == (ES == 1 ? 1 : 0), "codes have scales");
+  constexpr int QES = ES == 1 ? 2 : ES;   // bytes per element of the queries
   constexpr int ROWB = D * ES, CH = ROWB / 16, EPC = 16 / ES, W = kFusedWaves, T = W * 64;
   static_assert(NT <= 32, "a wave's tile masks are collected one per lane, its keys in one register vector per head");
   static_assert(GT <= W, "one wave scans one head's histogram");
@@ -763,6 +813,13 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
   v4u* mine = mine_all + wave * 64 * CH;
   const int sw = swz<CH>(lane);
   v4u regs[CH];
+  uint32_t unit = 0;   // scale byte of the row that this lane scores (see score_kernel)
+  auto fetch_unit = [&](int r0) {
+    if constexpr (ES == 1) {
+      const KeyScales sc = scales_of(scales...);
+      unit = sc.at[g * sc.head + scale_slot(kv0, b, sc.shift) + (min(r0 + lane, L - 1) >> sc.shift)];
+    }
+  };
   auto fetch = [&](int r0) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -770,20 +827,20 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
       regs[i] = load_once(base + row * row_pitch);
     }
   };
-  if (ntiles > 0) fetch(first);
+  if (ntiles > 0) { fetch(first); fetch_unit(first); }
 
   for (int t = tid; t < GT * kBinsA; t += T) hist_a[t] = 0;
   {   // block sums of this KV head's query heads, ascending rows (as in score_kernel)
     const int nq = q1 - q0;
-    const int64_t qpitch = s.q_tok * ES;
+    const int64_t qpitch = s.q_tok * QES;
     auto widen = [](const char* p) -> float {
-      if constexpr (ES == 2)
+      if constexpr (QES == 2)
         return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
       else
         return *reinterpret_cast<const float*>(p);
     };
     for (int e = tid; e < GT * D; e += T) {
-      const char* p = q + (int64_t(q0) * s.q_tok + int64_t(g * GT + e / D) * s.q_head + e % D) * ES;
+      const char* p = q + (int64_t(q0) * s.q_tok + int64_t(g * GT + e / D) * s.q_head + e % D) * QES;
       float a = 0.0f;
       int i = 0;
       for (; i + 32 <= nq; i += 32) {
@@ -820,7 +877,8 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
       const int f = i * 64 + lane, row = f / CH, c = f % CH;
       mine[row * CH + (c ^ swz<CH>(row))] = regs[i];
     }
-    if (it + 1 < ntiles) fetch(r0 + 64);
+    const uint32_t unit_now = unit;
+    if (it + 1 < ntiles) { fetch(r0 + 64); fetch_unit(r0 + 64); }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -831,17 +889,15 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
       constexpr int c = decltype(cc)::value;
       const v4u x = mine[lane * CH + (c ^ sw)];
       float kv[EPC];
-      if constexpr (ES == 2) {
-        kv[0] = bf16_lo(x.x); kv[1] = bf16_hi(x.x); kv[2] = bf16_lo(x.y); kv[3] = bf16_hi(x.y);
-        kv[4] = bf16_lo(x.z); kv[5] = bf16_hi(x.z); kv[6] = bf16_lo(x.w); kv[7] = bf16_hi(x.w);
-      } else {
-        kv[0] = __uint_as_float(x.x); kv[1] = __uint_as_float(x.y);
-        kv[2] = __uint_as_float(x.z); kv[3] = __uint_as_float(x.w);
-      }
+      widen_chunk<ES>(x, kv);
 #pragma unroll
-      for (int t = 0; t < GT; ++t) acc[t] = fma_row_bcast<(c * EPC) % 16, EPC>(acc[t], vq[t][(c * EPC) / 16], kv);
+      for (int t = 0; t < GT; ++t) acc[t] = fma_chunk<(c * EPC) % 16, EPC>(acc[t], vq[t][(c * EPC) / 16], kv);
     };
     for_each_index(chunk, std::make_integer_sequence<int, CH>{});
+    if constexpr (ES == 1) {
+#pragma unroll
+      for (int t = 0; t < GT; ++t) acc[t] = acc[t] * scale_of(unit_now);
+    }
     const bool valid = r0 + lane < Lc;
     uint32_t key[GT];
 #pragma unroll
@@ -1086,9 +1142,9 @@ SelectPlan plan_select(const Shape& s) {
   return p;
 }
 
-template <int ES, int D>
+template <int ES, int D, typename... Scales>
 static hipError_t launch_score(const Shape& s, const void* k, const void* q, const int32_t* cu_q,
-                               const int32_t* cu_kv, const int32_t* cu_k, float* scores, hipStream_t st) {
+                               const int32_t* cu_kv, const int32_t* cu_k, float* scores, hipStream_t st, Scales... scales) {
   // (Dealing a sequence's tiles out evenly over its workgroups' waves instead of in blocks cost 1 to 4 %.)
   static_assert(kScoreRowsPerBlock == 256, "dllm_rule_score_tiles counts in workgroups of four tiles");
   const int tpw = dllm_rule_score_tiles(s.batch, s.total_kv, s.max_kv, s.hkv, s.group, D * ES);
@@ -1101,17 +1157,17 @@ static hipError_t launch_score(const Shape& s, const void* k, const void* q, con
     const hipError_t ea = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                               hipFuncAttributeMaxDynamicSharedMemorySize, int(sums_bytes));
     if (ea != hipSuccess) return ea;
-    kernel<<<grid, block, sums_bytes, st>>>(kp, qp, cu_q, cu_kv, cu_k, scores, tpw, s DLLM_CHECK_PASS);
+    kernel<<<grid, block, sums_bytes, st>>>(kp, qp, cu_q, cu_kv, cu_k, scores, tpw, s, scales... DLLM_CHECK_PASS);
     return hipGetLastError();
   };
   if (streams_once(s, ES)) {
-    if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, true>);
-    if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, true>);
-    return launch(score_kernel<ES, D, 1, true>);
+    if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, true, Scales...>);
+    if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, true, Scales...>);
+    return launch(score_kernel<ES, D, 1, true, Scales...>);
   }
-  if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, false>);
-  if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, false>);
-  return launch(score_kernel<ES, D, 1, false>);
+  if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, false, Scales...>);
+  if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, false, Scales...>);
+  return launch(score_kernel<ES, D, 1, false, Scales...>);
 }
 
 static std::atomic<int32_t> g_select_form{DLLM_SELECT_FORM_AUTO};
@@ -1122,11 +1178,11 @@ int32_t set_select_form(int32_t form) {
 }
 
 // Shapes select_fused_kernel can take.
-static bool fused_can(const Shape& s, dllm_dtype dt, int32_t pool_w, int32_t head_sum) {
+static bool fused_can(const Shape& s, int es, int32_t pool_w, int32_t head_sum) {
   (void)pool_w;   // (any window the call accepts)
   if (head_sum) return false;
   if (s.group != 1 && s.group != 2 && s.group != 4) return false;
-  if (s.d * (dt == DLLM_BF16 ? 2 : 4) > 256) return false;
+  if (s.d * es > 256) return false;
   return s.max_kv <= kFusedWaves * kFusedTiles * 64;
 }
 // ... and where it pays (measured on batches of equal lists, 1 to 4 query heads per KV head, lists of
@@ -1164,8 +1220,8 @@ static int compute_units() {
 // against 9.1 / 9.2 / 10.1).  The block's queries cost both forms alike (1 / 32 / 256, 32 heads x 128, one of 256 6.3 / 6.8 / 9.5 against
 // 8.3 / 8.5 / 11.2) and are not priced.  Over 2361 calls measured in both forms the choice is 0.18 % above the better one in
 // the mean, 18 % at most (four query heads per KV head and blocks of 256 queries, where one launch would win).
-static bool fused_pays_short(const Shape& s, dllm_dtype dt, int32_t pool_w) {
-  const double row = s.d * (dt == DLLM_BF16 ? 2 : 4), mb = double(s.total_kv) * s.hkv * row * 1e-6, pooled = pool_w > 1;
+static bool fused_pays_short(const Shape& s, int es, int32_t pool_w) {
+  const double row = s.d * es, mb = double(s.total_kv) * s.hkv * row * 1e-6, pooled = pool_w > 1;
   const double wider = std::max(0, pool_w / 2 - 1);   // positions on either side beyond the first
   const int nt = (s.max_kv + 63) / 64, per_wave = (nt + kFusedWaves - 1) / kFusedWaves;
   const int per_simd = nt > kFusedWaves / 2 * per_wave ? 2 * per_wave : per_wave;   // tiles the busiest SIMD scores
@@ -1176,19 +1232,19 @@ static bool fused_pays_short(const Shape& s, dllm_dtype dt, int32_t pool_w) {
   two += 0.4 * pooled + 0.06 * wider * ((s.max_kv + kTopkThreads - 1) / kTopkThreads);
   return one < two;
 }
-static bool fused_pays(const Shape& s, dllm_dtype dt, int32_t pool_w) {
+static bool fused_pays(const Shape& s, int es, int32_t pool_w) {
   const int64_t pairs = int64_t(s.batch) * s.hkv, cus = compute_units();
-  if (pairs <= cus && s.max_kv <= kFusedWaves * kFusedTilesShort * 64) return fused_pays_short(s, dt, pool_w);
+  if (pairs <= cus && s.max_kv <= kFusedWaves * kFusedTilesShort * 64) return fused_pays_short(s, es, pool_w);
   const int64_t rounds = (pairs + cus - 1) / cus;
   const bool full = rounds == 1 ? 4 * pairs >= 3 * cus : 5 * pairs >= 4 * rounds * cus;
   const bool even = 4 * int64_t(s.total_kv) >= 3 * int64_t(s.batch) * s.max_kv;
   return full && even;
 }
 
-template <int ES, int D>
+template <int ES, int D, typename... Scales>
 static hipError_t launch_fused(const Shape& s, const void* k, const void* q, const int32_t* cu_q,
                                const int32_t* cu_kv, const int32_t* cu_k, int32_t total_k, int32_t forced_tail,
-                               int32_t pool_w, int32_t* idx_out, hipStream_t st) {
+                               int32_t pool_w, int32_t* idx_out, hipStream_t st, Scales... scales) {
   const char *kp = static_cast<const char*>(k), *qp = static_cast<const char*>(q);
   auto launch = [&](auto kernel, size_t lds) -> hipError_t {
     const hipError_t ea = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
@@ -1196,47 +1252,33 @@ static hipError_t launch_fused(const Shape& s, const void* k, const void* q, con
     if (ea != hipSuccess) return ea;
     const int32_t ranked = s.batch <= 64 && int64_t(s.batch) * s.hkv > compute_units() ? 1 : 0;
     kernel<<<dim3(s.batch * s.hkv), dim3(kFusedWaves * 64), lds, st>>>(kp, qp, cu_q, cu_kv, cu_k, total_k, forced_tail,
-                                                                       pool_w, ranked, idx_out, s DLLM_CHECK_PASS);
+                                                                       pool_w, ranked, idx_out, s, scales... DLLM_CHECK_PASS);
     return hipGetLastError();
   };
   auto pick = [&](auto tiles) -> hipError_t {
     constexpr int NT = decltype(tiles)::value;
-    if (s.group == 4) return launch(select_fused_kernel<ES, D, 4, NT>, FusedLds<ES, D, 4, NT>::bytes);
-    if (s.group == 2) return launch(select_fused_kernel<ES, D, 2, NT>, FusedLds<ES, D, 2, NT>::bytes);
-    return launch(select_fused_kernel<ES, D, 1, NT>, FusedLds<ES, D, 1, NT>::bytes);
+    if (s.group == 4) return launch(select_fused_kernel<ES, D, 4, NT, Scales...>, FusedLds<ES, D, 4, NT>::bytes);
+    if (s.group == 2) return launch(select_fused_kernel<ES, D, 2, NT, Scales...>, FusedLds<ES, D, 2, NT>::bytes);
+    return launch(select_fused_kernel<ES, D, 1, NT, Scales...>, FusedLds<ES, D, 1, NT>::bytes);
   };
   // A wave ranks all the tiles its registers hold, also those the list does not have.
   if (s.max_kv <= kFusedWaves * kFusedTilesShort * 64) return pick(std::integral_constant<int, kFusedTilesShort>{});
   return pick(std::integral_constant<int, kFusedTiles>{});
 }
 
-int32_t select_form_of(const Shape& s, dllm_dtype dt, int32_t pool_w, int32_t head_sum) {
+int32_t select_form_of(const Shape& s, int es, int32_t pool_w, int32_t head_sum) {
   const int32_t form = g_select_form.load();
-  const bool one = form != DLLM_SELECT_FORM_TWO_LAUNCHES && fused_can(s, dt, pool_w, head_sum) &&
-                   (form == DLLM_SELECT_FORM_ONE_LAUNCH || fused_pays(s, dt, pool_w));
+  const bool one = form != DLLM_SELECT_FORM_TWO_LAUNCHES && fused_can(s, es, pool_w, head_sum) &&
+                   (form == DLLM_SELECT_FORM_ONE_LAUNCH || fused_pays(s, es, pool_w));
   return one ? DLLM_SELECT_FORM_ONE_LAUNCH : DLLM_SELECT_FORM_TWO_LAUNCHES;
 }
 
-hipError_t launch_select(const Shape& s, dllm_dtype dt, const void* q, const void* k, const int32_t* cu_q,
-                         const int32_t* cu_kv, const int32_t* cu_k, int32_t total_k, int32_t max_k,
-                         int32_t pool_w, int32_t forced_tail, int32_t head_sum, int32_t* idx_out, void* ws,
-                         hipStream_t st) {
-  (void)max_k;
-  if (select_form_of(s, dt, pool_w, head_sum) == DLLM_SELECT_FORM_ONE_LAUNCH)
-    return dt == DLLM_BF16 ? (s.d == 128 ? launch_fused<2, 128>(s, k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st)
-                                         : launch_fused<2, 64>(s, k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st))
-                           : launch_fused<4, 64>(s, k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st);
-  const SelectPlan p = plan_select(s);
-  float* scores = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_scores);
+// the ranking launches over the scores (or, with head_sum, over their sums) that lie in the workspace
+static hipError_t launch_ranking(const Shape& s, const SelectPlan& p, const int32_t* cu_kv, const int32_t* cu_k, int32_t total_k,
+                                 int32_t pool_w, int32_t forced_tail, int32_t head_sum, int32_t* idx_out, void* ws,
+                                 hipStream_t st) {
+  const float* scores = reinterpret_cast<const float*>(static_cast<char*>(ws) + p.off_scores);
   hipError_t e;
-  if (dt == DLLM_BF16)
-    e = s.d == 128 ? launch_score<2, 128>(s, k, q, cu_q, cu_kv, cu_k, scores, st)
-                   : launch_score<2, 64>(s, k, q, cu_q, cu_kv, cu_k, scores, st);
-  else
-    e = s.d == 128 ? launch_score<4, 128>(s, k, q, cu_q, cu_kv, cu_k, scores, st)
-                   : launch_score<4, 64>(s, k, q, cu_q, cu_kv, cu_k, scores, st);
-  if (e != hipSuccess) return e;
-
   const float* ranked = scores;
   if (head_sum) {   // sum (pooled) scores over the heads first; the top-k then ranks one plain row per sequence
     float* summed = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_summed);
@@ -1276,6 +1318,43 @@ hipError_t launch_select(const Shape& s, dllm_dtype dt, const void* q, const voi
   topk_kernel<<<grid, kTopkThreads, lds, st>>>(
       ranked, cu_kv, cu_k, s.total_kv, total_k, pool_w, lpad, forced_tail, head_sum, s.hq, idx_out DLLM_CHECK_PASS);
   return hipGetLastError();
+}
+
+hipError_t launch_select(const Shape& s, dllm_dtype dt, const void* q, const void* k, const int32_t* cu_q,
+                         const int32_t* cu_kv, const int32_t* cu_k, int32_t total_k, int32_t max_k,
+                         int32_t pool_w, int32_t forced_tail, int32_t head_sum, int32_t* idx_out, void* ws,
+                         hipStream_t st) {
+  (void)max_k;
+  if (select_form_of(s, dt == DLLM_BF16 ? 2 : 4, pool_w, head_sum) == DLLM_SELECT_FORM_ONE_LAUNCH)
+    return dt == DLLM_BF16 ? (s.d == 128 ? launch_fused<2, 128>(s, k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st)
+                                         : launch_fused<2, 64>(s, k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st))
+                           : launch_fused<4, 64>(s, k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st);
+  const SelectPlan p = plan_select(s);
+  float* scores = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_scores);
+  hipError_t e;
+  if (dt == DLLM_BF16)
+    e = s.d == 128 ? launch_score<2, 128>(s, k, q, cu_q, cu_kv, cu_k, scores, st)
+                   : launch_score<2, 64>(s, k, q, cu_q, cu_kv, cu_k, scores, st);
+  else
+    e = s.d == 128 ? launch_score<4, 128>(s, k, q, cu_q, cu_kv, cu_k, scores, st)
+                   : launch_score<4, 64>(s, k, q, cu_q, cu_kv, cu_k, scores, st);
+  if (e != hipSuccess) return e;
+  return launch_ranking(s, p, cu_kv, cu_k, total_k, pool_w, forced_tail, head_sum, idx_out, ws, st);
+}
+
+hipError_t launch_select_cached(const Shape& s, const CacheView& c, const void* q, const int32_t* cu_q, const int32_t* cu_kv,
+                                const int32_t* cu_k, int32_t total_k, int32_t pool_w, int32_t forced_tail, int32_t head_sum,
+                                int32_t* idx_out, void* ws, hipStream_t st) {
+  const KeyScales scales = {c.ks, c.scale_head, c.shift};
+  if (select_form_of(s, 1, pool_w, head_sum) == DLLM_SELECT_FORM_ONE_LAUNCH)
+    return s.d == 128 ? launch_fused<1, 128>(s, c.k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st, scales)
+                      : launch_fused<1, 64>(s, c.k, q, cu_q, cu_kv, cu_k, total_k, forced_tail, pool_w, idx_out, st, scales);
+  const SelectPlan p = plan_select(s);
+  float* scores = reinterpret_cast<float*>(static_cast<char*>(ws) + p.off_scores);
+  const hipError_t e = s.d == 128 ? launch_score<1, 128>(s, c.k, q, cu_q, cu_kv, cu_k, scores, st, scales)
+                                  : launch_score<1, 64>(s, c.k, q, cu_q, cu_kv, cu_k, scores, st, scales);
+  if (e != hipSuccess) return e;
+  return launch_ranking(s, p, cu_kv, cu_k, total_k, pool_w, forced_tail, head_sum, idx_out, ws, st);
 }
 
 }  // namespace dllm

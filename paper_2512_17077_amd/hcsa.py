@@ -32,6 +32,9 @@ EXPORTS = [
     "dllm_hcsa_attend_workspace", "dllm_hcsa_attend", "dllm_hcsa_attend_form_of",
     "dllm_dense_refresh_attend_workspace", "dllm_dense_refresh_attend",
     "dllm_hcsa_pack", "dllm_hcsa_precondition_errors",
+    "dllm_hcsa_cache_scale_slots", "dllm_hcsa_cache_write", "dllm_hcsa_cache_read",
+    "dllm_hcsa_select_cached_workspace", "dllm_hcsa_select_cached",
+    "dllm_hcsa_attend_cached_workspace", "dllm_hcsa_attend_cached",
     "dllm_last_error", "dllm_hcsa_version",
 ]
 DLLM_CHECK_CU_Q, DLLM_CHECK_CU_KV, DLLM_CHECK_CU_K, DLLM_CHECK_K_OVER_L, DLLM_CHECK_FORCED, DLLM_CHECK_IDX = 1, 2, 4, 8, 16, 32
@@ -59,6 +62,20 @@ class DllmBatch(ctypes.Structure):
         ("max_q", ctypes.c_int32),
         ("max_kv", ctypes.c_int32),
         ("softmax_scale", ctypes.c_float),
+    ]
+
+
+class DllmCache(ctypes.Structure):
+    """Mirror of `dllm_cache`."""
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("stride_tok", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+        ("scale_stride_head", ctypes.c_int64),
+        ("scale_block", ctypes.c_int32),
     ]
 
 
@@ -107,6 +124,21 @@ def lib() -> ctypes.CDLL:
         L.dllm_hcsa_pack.argtypes = [P, vp, vp, i32, i32, vp, vp, vp]
         L.dllm_hcsa_precondition_errors.restype = ctypes.c_int
         L.dllm_hcsa_precondition_errors.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
+        C, i64 = ctypes.POINTER(DllmCache), ctypes.c_int64
+        L.dllm_hcsa_cache_scale_slots.restype = i64
+        L.dllm_hcsa_cache_scale_slots.argtypes = [i32, i32, i32]
+        L.dllm_hcsa_cache_write.restype = ctypes.c_int
+        L.dllm_hcsa_cache_write.argtypes = [P, C, vp, i32, i32, vp, vp]
+        L.dllm_hcsa_cache_read.restype = ctypes.c_int
+        L.dllm_hcsa_cache_read.argtypes = [P, C, vp, i32, i32, vp, vp, vp, vp]
+        L.dllm_hcsa_select_cached_workspace.restype = sz
+        L.dllm_hcsa_select_cached_workspace.argtypes = [P, C, i32]
+        L.dllm_hcsa_select_cached.restype = ctypes.c_int
+        L.dllm_hcsa_select_cached.argtypes = [P, C, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+        L.dllm_hcsa_attend_cached_workspace.restype = sz
+        L.dllm_hcsa_attend_cached_workspace.argtypes = [P, C, i32]
+        L.dllm_hcsa_attend_cached.restype = ctypes.c_int
+        L.dllm_hcsa_attend_cached.argtypes = [P, C, vp, vp, i32, i32, vp, vp, sz, vp]
         L.dllm_last_error.restype = ctypes.c_char_p
         L.dllm_last_error.argtypes = []
         L.dllm_hcsa_version.restype = i32
@@ -284,3 +316,143 @@ def make_packed_batch(q: torch.Tensor, k_packed: torch.Tensor, v_packed: torch.T
     query head, rows of a head contiguous, sequence b owning list positions cu_k[b] .. cu_k[b+1]-1."""
     assert k_packed.dim() == 3 and k_packed.is_contiguous() and v_packed.is_contiguous()
     return make_batch(q, k_packed.transpose(0, 1), v_packed.transpose(0, 1), cu_q, cu_k, max_q, max_k, softmax_scale)
+
+
+# ---------------------------------------------------------------- the 8-bit cache
+def cache_scale_slots(total_kv: int, batch: int, scale_block: int) -> int:
+    """Entries of one head's row of scales in a cache of `batch` sequences with total_kv tokens together."""
+    n = int(lib().dllm_hcsa_cache_scale_slots(int(total_kv), int(batch), int(scale_block)))
+    if n < 0:
+        raise ValueError(f"no cache has total_kv={total_kv}, batch={batch}, scale_block={scale_block} (16, 32 or 64)")
+    return n
+
+
+def make_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, scale_block: int) -> DllmCache:
+    """Describe codes k/v [total_kv, Hkv, D] (float8_e4m3fn or uint8, last dim contiguous) and their scale bytes [Hkv, slots]
+    (uint8, last dim contiguous) to the library.  Zero the memory of a new cache."""
+    assert k.dim() == 3 and k.shape == v.shape and k.stride() == v.stride() and k.stride(2) == 1
+    assert k.dtype == v.dtype and k.dtype in (torch.uint8, torch.float8_e4m3fn)
+    assert k_scale.dtype == v_scale.dtype == torch.uint8 and k_scale.dim() == 2 and k_scale.shape[0] == k.shape[1]
+    assert k_scale.shape == v_scale.shape and k_scale.stride() == v_scale.stride() and k_scale.stride(1) == 1
+    assert k.device == v.device == k_scale.device == v_scale.device
+    assert scale_block in (16, 32, 64)
+    c = DllmCache()
+    c.k, c.v, c.k_scale, c.v_scale = k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
+    c.stride_tok, c.stride_head = k.stride(0), k.stride(1)
+    # a single head's row is as long as its scales say, whatever stride a tensor of one row has
+    c.scale_stride_head = k_scale.stride(0) if k_scale.shape[0] > 1 else k_scale.shape[1]
+    c.scale_block = int(scale_block)
+    # (not part of the C structure: the tensors stay alive with their descriptor; for the checks below)
+    c.tensors = (k, v, k_scale, v_scale)
+    c.shape = tuple(k.shape)
+    c.slots = int(k_scale.shape[1])
+    return c
+
+
+def make_cached_batch(q: torch.Tensor, cu_q: torch.Tensor, cu_kv: torch.Tensor, total_kv: int, n_kv_heads: int, max_q: int,
+                      max_kv: int, softmax_scale: float) -> DllmBatch:
+    """Describe packed queries q [total_q,Hq,D] and the sequences of a cache (select_cached, attend_cached)."""
+    assert q.dim() == 3 and q.stride(2) == 1 and cu_q.dtype == torch.int32 and cu_kv.dtype == torch.int32
+    b = DllmBatch()
+    b.dtype = {torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16}[q.dtype]
+    b.batch = cu_q.numel() - 1
+    assert cu_kv.numel() == b.batch + 1
+    b.n_q_heads, b.n_kv_heads, b.head_dim = q.shape[1], int(n_kv_heads), q.shape[2]
+    b.q = q.data_ptr()
+    b.q_stride_tok, b.q_stride_head = q.stride(0), q.stride(1)
+    b.cu_q, b.cu_kv = cu_q.data_ptr(), cu_kv.data_ptr()
+    b.total_q, b.total_kv = q.shape[0], int(total_kv)
+    b.max_q, b.max_kv = int(max_q), int(max_kv)
+    b.softmax_scale = float(softmax_scale)
+    b.tensors = (q, cu_q, cu_kv)   # (as in make_cache)
+    return b
+
+
+def make_rows_batch(k: torch.Tensor, v: torch.Tensor, cu_kv: torch.Tensor, total_kv: int, max_kv: int) -> DllmBatch:
+    """Describe rows k/v [total_rows,Hkv,D] (bf16 or fp32) and the sequences of the cache that they go to or come from."""
+    assert k.dim() == 3 and k.stride(2) == 1 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
+    assert cu_kv.dtype == torch.int32
+    b = DllmBatch()
+    b.dtype = {torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16}[k.dtype]
+    b.batch = cu_kv.numel() - 1
+    b.n_q_heads = b.n_kv_heads = k.shape[1]
+    b.head_dim = k.shape[2]
+    b.k, b.v = k.data_ptr(), v.data_ptr()
+    b.kv_stride_tok, b.kv_stride_head = k.stride(0), k.stride(1)
+    b.cu_kv = cu_kv.data_ptr()
+    b.total_kv, b.max_kv = int(total_kv), int(max_kv)
+    b.tensors = (k, v, cu_kv)   # (as in make_cache)
+    b.rows = int(k.shape[0])
+    return b
+
+
+def _check_cache(batch: DllmBatch, cache: DllmCache):
+    assert cache.shape == (batch.total_kv, batch.n_kv_heads, batch.head_dim), "the cache has another shape than the batch says"
+    assert cache.slots >= (batch.total_kv // cache.scale_block) + batch.batch, "too few scales (cache_scale_slots)"
+
+
+def _check_ranges(batch: DllmBatch, cu_rows, total_rows, at):
+    if cu_rows is None:
+        assert at is None and batch.rows >= batch.total_kv, "without cu_rows all rows are moved"
+        return batch.total_kv
+    assert cu_rows.dtype == torch.int32 and cu_rows.numel() == batch.batch + 1
+    assert at is None or (at.dtype == torch.int32 and at.numel() == batch.batch and at.is_contiguous())
+    assert batch.rows >= int(total_rows), "fewer rows than total_rows"
+    return int(total_rows)
+
+
+def dllm_hcsa_cache_write(batch: DllmBatch, cache: DllmCache, cu_rows: Optional[torch.Tensor] = None, total_rows: int = 0,
+                          max_rows: int = 0, at: Optional[torch.Tensor] = None, stream=None) -> DllmCache:
+    """Quantise the rows of `batch` (make_rows_batch) into the cache: cu_rows[b] .. cu_rows[b+1]-1 to positions at[b] .. of
+    sequence b (at None: its last ones), or every sequence whole (cu_rows None)."""
+    _check_cache(batch, cache)
+    total_rows = _check_ranges(batch, cu_rows, total_rows, at)
+    _raise(lib().dllm_hcsa_cache_write(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, int(max_rows),
+                                       _ptr(at), _stream(stream)))
+    return cache
+
+
+def dllm_hcsa_cache_read(batch: DllmBatch, cache: DllmCache, k_out: torch.Tensor, v_out: torch.Tensor,
+                         cu_rows: Optional[torch.Tensor] = None, total_rows: int = 0, max_rows: int = 0,
+                         at: Optional[torch.Tensor] = None, stream=None):
+    """Read rows of the cache back into k_out / v_out, the tensors that `batch` describes (make_rows_batch)."""
+    _check_cache(batch, cache)
+    assert (k_out.data_ptr(), v_out.data_ptr()) == (batch.k or 0, batch.v or 0), "batch describes other tensors"
+    total_rows = _check_ranges(batch, cu_rows, total_rows, at)
+    _raise(lib().dllm_hcsa_cache_read(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, int(max_rows),
+                                      _ptr(at), _ptr(k_out), _ptr(v_out), _stream(stream)))
+    return k_out, v_out
+
+
+def dllm_hcsa_select_cached_workspace(batch: DllmBatch, cache: DllmCache, max_k: int) -> int:
+    return int(lib().dllm_hcsa_select_cached_workspace(ctypes.byref(batch), ctypes.byref(cache), int(max_k)))
+
+
+def dllm_hcsa_select_cached(batch: DllmBatch, cache: DllmCache, cu_k: torch.Tensor, total_k: int, max_k: int,
+                            idx_out: torch.Tensor, pool_w: int = 1, forced_tail: int = 0, head_sum: bool = False,
+                            workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Selection over the cached K (batch: make_cached_batch); fills idx_out [Hq, total_k] (int32, device)."""
+    _check_cache(batch, cache)
+    if workspace is None:
+        workspace = _workspace(dllm_hcsa_select_cached_workspace(batch, cache, max_k), idx_out.device)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _raise(lib().dllm_hcsa_select_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_k), int(total_k), int(max_k),
+                                         int(pool_w), int(forced_tail), int(bool(head_sum)), _ptr(idx_out), _ptr(workspace),
+                                         nbytes, _stream(stream)))
+    return idx_out
+
+
+def dllm_hcsa_attend_cached_workspace(batch: DllmBatch, cache: DllmCache, max_k: int) -> int:
+    return int(lib().dllm_hcsa_attend_cached_workspace(ctypes.byref(batch), ctypes.byref(cache), int(max_k)))
+
+
+def dllm_hcsa_attend_cached(batch: DllmBatch, cache: DllmCache, idx: Optional[torch.Tensor], cu_k: torch.Tensor, total_k: int,
+                            max_k: int, o: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention over the cache: every head over its own list, or (idx None) all heads over the first rows of each sequence."""
+    _check_cache(batch, cache)
+    if workspace is None:
+        workspace = _workspace(dllm_hcsa_attend_cached_workspace(batch, cache, max_k), o.device)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _raise(lib().dllm_hcsa_attend_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(idx), _ptr(cu_k), int(total_k),
+                                         int(max_k), _ptr(o), _ptr(workspace), nbytes, _stream(stream)))
+    return o

@@ -1,0 +1,694 @@
+"""The 8-bit KV cache on the GPU: rows written and read back, selection and attention over it, alone and in the order in which
+a denoising step or a decoding step makes them, against plain 64-bit references of the definition.
+
+Codes, scales, values read back and kept positions have to be equal.  Outputs of attention: the kernels round each probability
+p and each output once to bf16 (half a step is 2^-8 of the value) and keep the rest in fp32.  With p' = p (1 + d), |d| <= 2^-8,
+    sum p' v / sum p' - o = sum (p' - p) (v - o) / sum p',   at most 2^-8 / (1 - 2^-8) * A,   A = sum p |v - o| / sum p;
+fp32 sums of D products give a score an error of at most (D + 2) 2^-24 S, S = scale * sum |q_d k_d|, exp2 and its argument (up
+to Z = |score| log2 e in size, twice: score and maximum) 2^-22 + 2^-22 Z, which again change p by a factor; accumulating n terms in
+order adds n 2^-24 of sum p |v|; then 2^-8 |o| for the output.  All of it is computed per output below."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2512_17077_amd import hcsa, synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def say(msg):
+    print(msg, flush=True)
+
+
+# ---------------------------------------------------------------- the definition, on the CPU
+def code_values():
+    out = np.empty(256)
+    for c in range(256):
+        e, m = (c >> 3) & 15, c & 7
+        x = math.ldexp(m, -9) if e == 0 else math.ldexp(8 + m, e - 10)
+        out[c] = math.nan if (c & 127) == 127 else -x if c & 128 else x
+    return out
+
+
+VALUES = code_values()
+UP = VALUES[:127]                       # 0 .. 448, ascending with the code
+HALF = (UP[:-1] + UP[1:]) / 2           # borders between neighbours, exact
+
+
+def encode(x, scale_byte):
+    """Codes of x (fp64) under a scale: the nearest value, ties to the even code; NaN and infinities 0x7f with the sign."""
+    y = np.abs(x) * math.ldexp(1.0, 127 - max(int(scale_byte), 1))
+    sign = np.where(np.signbit(x), 128, 0)
+    y = np.where(np.isfinite(x), np.minimum(y, 448.0), 0.0)
+    i = np.searchsorted(HALF, y, side="left")            # borders below y: a tie stays low
+    tie = (i < len(HALF)) & (y == HALF[np.minimum(i, len(HALF) - 1)]) & (i % 2 == 1)
+    code = i + tie
+    return (np.where(np.isfinite(x), code, 127) | sign).astype(np.uint8)
+
+
+def scale_for(x):
+    m = np.abs(x[np.isfinite(x)])
+    most = float(m.max()) if m.size else 0.0
+    if most == 0.0:
+        return 0
+    f, e = math.frexp(most / 448.0)     # most / 448 <= 2^k: k = e, or e - 1 if it is a power of two (448 = 7 * 64: tested exactly)
+    k = e - 1 if most == math.ldexp(448.0, e - 1) else e
+    return min(max(k + 127, 32), 246)
+
+
+class Cache:
+    """A cache on the GPU, and what it has to hold as numpy arrays."""
+
+    def __init__(self, lens, hkv, d, block, layout="token", fill=0):
+        self.lens, self.hkv, self.d, self.block = list(lens), hkv, d, block
+        self.cu = np.concatenate([[0], np.cumsum(self.lens)]).astype(np.int32)
+        self.total = int(self.cu[-1])
+        self.slots = hcsa.cache_scale_slots(self.total, len(self.lens), block)
+        if layout == "token":
+            shape, view = (self.total, hkv, d), lambda t: t
+        elif layout == "head":
+            shape, view = (hkv, self.total, d), lambda t: t.transpose(0, 1)
+        else:   # padded rows
+            shape, view = (self.total, hkv + 1, d + 16), lambda t: t[:, :hkv, :d]
+        self.raw = {x: torch.full(shape, fill, dtype=torch.uint8, device=DEV) for x in "kv"}
+        self.t = {x: view(self.raw[x]) for x in "kv"}
+        self.raw_s = {x: torch.full((hkv, self.slots + 3), fill, dtype=torch.uint8, device=DEV) for x in "kv"}
+        self.s = {x: self.raw_s[x][:, :self.slots + 2] for x in "kv"}
+        self.desc = hcsa.make_cache(self.t["k"], self.t["v"], self.s["k"], self.s["v"], block)
+        self.cu_t = torch.from_numpy(self.cu).to(DEV)
+        self.want = {x: np.full((self.total, hkv, d), fill, np.uint8) for x in "kv"}
+        self.want_s = {x: np.full((hkv, self.slots + 2), fill, np.uint8) for x in "kv"}
+
+    def slot(self, b, p):
+        return int(self.cu[b]) // self.block + b + p // self.block
+
+    def expect(self, x, rows, starts, counts):
+        """What a write of rows (fp64 [n, hkv, d]) to positions starts[b] .. of every sequence leaves."""
+        first = 0
+        for b, (at, n) in enumerate(zip(starts, counts)):
+            lo, hi = max(at, 0), min(at + n, self.lens[b])
+            for blk in range(lo // self.block, -(-hi // self.block)) if lo < hi else ():
+                b0, b1 = blk * self.block, min((blk + 1) * self.block, self.lens[b])
+                w0, w1 = max(lo, b0), min(hi, b1)
+                for g in range(self.hkv):
+                    new = rows[first + w0 - at:first + w1 - at, g]
+                    sl = self.slot(b, b0)
+                    old = int(self.want_s[x][g, sl]) if w1 - w0 < b1 - b0 else 0
+                    c = max(scale_for(new), old)
+                    g0 = int(self.cu[b])
+                    for p in range(b0, b1):
+                        if w0 <= p < w1:
+                            self.want[x][g0 + p, g] = encode(rows[first + p - at, g], c)
+                        elif c > old:
+                            stood = VALUES[self.want[x][g0 + p, g]] * math.ldexp(1.0, max(old, 1) - 127)
+                            self.want[x][g0 + p, g] = encode(stood, c)
+                    self.want_s[x][g, sl] = c
+            first += n
+
+    def write(self, k, v, starts=None, counts=None, pass_at=True):
+        """k, v: GPU tensors.  starts None: whole sequences."""
+        batch = hcsa.make_rows_batch(k, v, self.cu_t, self.total, max(self.lens, default=0))
+        if starts is None:
+            hcsa.dllm_hcsa_cache_write(batch, self.desc)
+            starts, counts = [0] * len(self.lens), self.lens
+        else:
+            cu = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device=DEV)
+            at = torch.tensor(starts, dtype=torch.int32, device=DEV) if pass_at else None
+            hcsa.dllm_hcsa_cache_write(batch, self.desc, cu, sum(counts), max(counts), at)
+        torch.cuda.synchronize()
+        for x, t in (("k", k), ("v", v)):
+            self.expect(x, t.double().cpu().numpy(), starts, counts)
+
+    def check(self):
+        for x in "kv":
+            got, want = self.t[x].cpu().numpy(), self.want[x]
+            nan = (got & 127 == 127) & (want & 127 == 127)
+            bad = np.argwhere((got != want) & ~nan)
+            assert len(bad) == 0, f"{x}: {len(bad)} codes differ, first at {bad[0]}: {got[tuple(bad[0])]} for {want[tuple(bad[0])]}"
+            gs = self.s[x].cpu().numpy()
+            assert np.array_equal(gs, self.want_s[x]), f"{x}: scales differ at {np.argwhere(gs != self.want_s[x])[:3]}"
+
+    def values(self, x):
+        """What the cache stands for, fp64 [total, hkv, d]."""
+        out = VALUES[self.want[x]]
+        for b, n in enumerate(self.lens):
+            for p in range(0, n, self.block):
+                u = np.ldexp(1.0, self.want_s[x][:, self.slot(b, p)].astype(int) - 127)
+                lo, hi = int(self.cu[b]) + p, int(self.cu[b]) + min(n, p + self.block)
+                out[lo:hi] *= u[None, :, None]
+        return out
+
+    def take(self):
+        """Takes what is on the GPU as what is held (for caches too large to quantise on the CPU)."""
+        for x in "kv":
+            self.want[x], self.want_s[x] = self.t[x].cpu().numpy(), self.s[x].cpu().numpy()
+
+
+def normal(n, h, d, dtype, seed, salient=0.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, h, d), generator=g)
+    if salient:
+        x = torch.where(torch.rand((n, h, 1), generator=g) < salient, 4.0 * x, x)
+    return x.to(dtype).to(DEV)
+
+
+def filled(lens, hkv, d, block, seed, layout="token", salient=0.05):
+    c = Cache(lens, hkv, d, block, layout)
+    k, v = normal(c.total, hkv, d, torch.bfloat16, seed, salient), normal(c.total, hkv, d, torch.bfloat16, seed + 1)
+    batch = hcsa.make_rows_batch(k, v, c.cu_t, c.total, max(lens))
+    hcsa.dllm_hcsa_cache_write(batch, c.desc)
+    torch.cuda.synchronize()
+    c.take()
+    return c
+
+
+def cu32(x):
+    return np.concatenate([[0], np.cumsum(x)]).astype(np.int32)
+
+
+# ---------------------------------------------------------------- writing
+def test_the_reference_encodes_its_own_values():
+    assert np.array_equal(encode(VALUES[:127], 127), np.arange(127)) and np.array_equal(encode(-VALUES[1:127], 127), np.arange(129, 255))
+    assert scale_for(np.array([448.0])) == 127 and scale_for(np.array([448.1])) == 128 and scale_for(np.array([224.0])) == 126
+    assert scale_for(np.array([0.0, np.inf])) == 0 and scale_for(np.array([1e-40])) == 32 and scale_for(np.array([3e38])) == 246
+
+
+@pytest.mark.parametrize("block,d", [(16, 64), (32, 128), (64, 64)])
+def test_every_bf16_pattern_is_stored_as_the_definition_says(block, d):
+    """All 65536 patterns, in blocks of neighbours (one or two exponents each) and in blocks of everything but the largest."""
+    bits = torch.arange(65536, dtype=torch.int32)
+    for part in ("neighbours", "mixed", "small"):
+        order = bits
+        if part != "neighbours":
+            order = bits[torch.randperm(65536, generator=torch.Generator().manual_seed(7))]
+        if part == "small":   # finite values of magnitude below 2: their blocks have scales that resolve something
+            order = order[(order & 0x7FFF) < 0x4000]
+            order = order[:order.numel() // (block * d) * block * d]
+        x = order.to(torch.int16).view(torch.bfloat16).reshape(-1, 1, d).to(DEV)
+        say(f"patterns {part} block={block} d={d}")
+        c = Cache([x.shape[0]], 1, d, block)
+        c.write(x, x.flip(0).contiguous())
+        c.check()
+
+
+@pytest.mark.parametrize("block,d", [(16, 128), (32, 64), (64, 128)])
+def test_fp32_values_round_once(block, d):
+    """Random fp32 patterns, and values on and next to the borders between codes (a detour over bf16 would move them)."""
+    g = torch.Generator().manual_seed(11)
+    n = 128 * d
+    wild = torch.randint(-2 ** 31, 2 ** 31 - 1, (n,), generator=g, dtype=torch.int64).to(torch.int32).view(torch.float32)
+    half = torch.from_numpy(HALF.astype(np.float32))
+    near = torch.stack([half, torch.nextafter(half, half * 2), torch.nextafter(half, half * 0)], 1).reshape(-1)
+    near = near.repeat(n // near.numel() + 1)[:n].clone()
+    near[::97] = 448.0   # every block's scale is 1
+    near[1::2] *= -1
+    for name, x in (("wild", wild), ("borders", near)):
+        say(f"fp32 {name} block={block} d={d}")
+        x = x.reshape(-1, 1, d).to(DEV)
+        c = Cache([x.shape[0]], 1, d, block)
+        c.write(x, x.flip(0).contiguous())
+        c.check()
+
+
+@pytest.mark.parametrize("layout", ["token", "head", "padded"])
+@pytest.mark.parametrize("dtype,d,hkv,block", [(torch.bfloat16, 128, 3, 32), (torch.float32, 64, 2, 16), (torch.bfloat16, 64, 1, 64),
+                                               (torch.float32, 128, 5, 64), (torch.bfloat16, 128, 2, 16), (torch.float32, 64, 3, 32)])
+def test_whole_and_partial_writes_into_ragged_sequences(dtype, d, hkv, block, layout):
+    """Sequences of odd lengths, of one row and of none; then rows at odd places, larger, smaller, zero, across blocks, behind the
+    end and before the start; rows next to them, unused scales and the memory around the cache stay as they were."""
+    lens = [37, 1, 0, block, 2 * block + 1, block - 1, 100]
+    say(f"write {layout} {dtype} d={d} hkv={hkv} block={block}")
+    c = Cache(lens, hkv, d, block, layout)
+    k, v = normal(c.total, hkv, d, dtype, 1), normal(c.total, hkv, d, dtype, 2)
+    k[5] = 0
+    c.write(k, v)
+    c.check()
+    rng = np.random.default_rng(5)
+    for turn, gain in enumerate((1.0, 9.0, 300.0, 0.01, 0.0, 3e4)):
+        counts = [int(rng.integers(0, n + 1)) for n in lens]
+        starts = [int(rng.integers(0, n - m + 1)) for n, m in zip(lens, counts)]
+        if turn == 2:   # ranges that leave their sequence on either side
+            starts = [s - 3 if b % 2 else s + 2 for b, s in enumerate(starts)]
+        wide = torch.randn((sum(counts) + 4, hkv + 1, d), generator=torch.Generator().manual_seed(turn)).mul(gain).to(dtype).to(DEV)
+        k = wide[2:2 + sum(counts), :hkv]   # a strided view
+        v = wide.flip(0).contiguous()[2:2 + sum(counts), :hkv]
+        if sum(counts) and max(counts):
+            c.write(k, v, starts, counts)
+            c.check()
+            c.write(k, v, starts, counts)   # the same again changes nothing
+            c.check()
+    ends = [min(n, 7) for n in lens]   # at = None: the last rows
+    k = normal(sum(ends), hkv, d, dtype, 9)
+    c2 = [n - m for n, m in zip(lens, ends)]
+    c.write(k, k.clone(), c2, ends, pass_at=False)
+    c.check()
+    for x in "kv":
+        if layout == "padded":
+            assert int(c.raw[x][:, hkv:].max()) == 0 and int(c.raw[x][:, :, d:].max()) == 0
+        assert int(c.raw_s[x][:, c.slots:].max()) == 0
+
+
+def test_a_block_that_keeps_rows_keeps_nan_rows_too():
+    c = Cache([40], 2, 64, 32)
+    k = normal(40, 2, 64, torch.bfloat16, 3)
+    k[7, 0, 3], k[9, 1, 0], k[35, 0, 63] = math.nan, math.inf, -math.inf
+    c.write(k, k.clone())
+    c.check()
+    c.write(100 * k[10:12], -k[10:12], [10], [2])
+    c.check()
+    assert (c.want["k"][7, 0, 3] & 127) == 127 and (c.want["k"][9, 1, 0] & 127) == 127 and c.want["k"][35, 0, 63] == 255
+
+
+# ---------------------------------------------------------------- reading back
+@pytest.mark.parametrize("layout", ["token", "head"])
+@pytest.mark.parametrize("dtype,d,hkv,block", [(torch.bfloat16, 128, 3, 32), (torch.float32, 64, 2, 16), (torch.bfloat16, 64, 5, 64),
+                                               (torch.float32, 128, 1, 32)])
+def test_rows_read_back_are_code_times_scale(dtype, d, hkv, block, layout):
+    lens = [70, 0, 1, block, 129]
+    c = Cache(lens, hkv, d, block, layout)
+    k, v = normal(c.total, hkv, d, torch.float32, 1), normal(c.total, hkv, d, torch.float32, 2) * 1e-3
+    k[3, 0, 1], k[8] = math.nan, 0
+    c.write(k, v)
+    out = {x: torch.full((c.total + 2, hkv, d), 7.0, dtype=dtype, device=DEV) for x in "kv"}
+    mid = {x: t[1:-1] for x, t in out.items()}
+    batch = hcsa.make_rows_batch(mid["k"], mid["v"], c.cu_t, c.total, max(lens))
+    say(f"read {layout} {dtype} d={d}")
+    hcsa.dllm_hcsa_cache_read(batch, c.desc, mid["k"], mid["v"])
+    torch.cuda.synchronize()
+    for x in "kv":
+        got, want = mid[x].double().cpu().numpy(), c.values(x)
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.nan_to_num(got), np.nan_to_num(want))
+        assert (out[x][0] == 7).all() and (out[x][-1] == 7).all()
+    counts = [min(n, m) for n, m in zip(lens, (33, 5, 1, 2, 100))]
+    starts = [17, 0, 0, 3, 40]   # the last range leaves its sequence
+    cu, at = torch.from_numpy(cu32(counts)).to(DEV), torch.tensor(starts, dtype=torch.int32, device=DEV)
+    wide = {x: torch.full((sum(counts), hkv + 2, d), 7.0, dtype=dtype, device=DEV) for x in "kv"}
+    part = {x: t[:, 1:-1] for x, t in wide.items()}
+    batch = hcsa.make_rows_batch(part["k"], part["v"], c.cu_t, c.total, max(lens))
+    hcsa.dllm_hcsa_cache_read(batch, c.desc, part["k"], part["v"], cu, sum(counts), max(counts), at)
+    torch.cuda.synchronize()
+    for x in "kv":
+        full, want = c.values(x), np.full((sum(counts), hkv, d), 7.0)
+        first = 0
+        for b, (s, n) in enumerate(zip(starts, counts)):
+            m = max(0, min(n, lens[b] - s))
+            want[first:first + m] = full[int(c.cu[b]) + s:int(c.cu[b]) + s + m]
+            first += n
+        got = part[x].double().cpu().numpy()
+        assert np.array_equal(np.nan_to_num(got, nan=-5), np.nan_to_num(want, nan=-5))
+        assert (wide[x][:, 0] == 7).all() and (wide[x][:, -1] == 7).all()
+
+
+# ---------------------------------------------------------------- selection
+def read_back(c):
+    k, v = (torch.empty((c.total, c.hkv, c.d), dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    hcsa.dllm_hcsa_cache_read(hcsa.make_rows_batch(k, v, c.cu_t, c.total, max(c.lens)), c.desc, k, v)
+    return k, v
+
+
+def check_select(c, hq, qlens, keep, seed, pool_w=1, forced=0, head_sum=False, q=None):
+    cu_q, cu_k = cu32(qlens), cu32(keep)
+    q = normal(int(cu_q[-1]), hq, c.d, torch.bfloat16, seed) if q is None else q
+    k, _ = read_back(c)
+    args = (synth.to_bits(q.cpu()), synth.to_bits(k.cpu()), cu_q, c.cu, cu_k)
+    ref = oracle.select_ex(*args, pool_w, forced, head_sum)
+    batch = hcsa.make_cached_batch(q, torch.from_numpy(cu_q).to(DEV), c.cu_t, c.total, c.hkv, max(qlens), max(c.lens), 0.1)
+    cu_kt = torch.from_numpy(cu_k).to(DEV)
+    try:
+        for form in (hcsa.DLLM_SELECT_FORM_TWO_LAUNCHES, hcsa.DLLM_SELECT_FORM_ONE_LAUNCH, hcsa.DLLM_SELECT_FORM_AUTO):
+            hcsa.dllm_hcsa_set_select_form(form)
+            idx = torch.full((hq, int(cu_k[-1])), -7, dtype=torch.int32, device=DEV)
+            hcsa.dllm_hcsa_select_cached(batch, c.desc, cu_kt, int(cu_k[-1]), max(keep), idx, pool_w, forced, head_sum)
+            torch.cuda.synchronize()
+            got = idx.cpu().numpy()
+            assert np.array_equal(got, ref), f"form {form}: {int((got != ref).sum())} of {ref.size} positions differ"
+    finally:
+        hcsa.dllm_hcsa_set_select_form(hcsa.DLLM_SELECT_FORM_AUTO)
+    return ref
+
+
+@pytest.mark.parametrize("pool_w,forced,head_sum", [(1, 0, False), (3, 0, False), (5, 16, False), (1, 16, True), (3, 0, True), (63, 0, False)])
+@pytest.mark.parametrize("hq,hkv,d,block", [(4, 4, 128, 32), (8, 4, 64, 16), (8, 2, 128, 64), (6, 2, 64, 32), (8, 1, 128, 16), (5, 5, 64, 64)])
+def test_kept_positions_are_those_of_the_values_read_back(hq, hkv, d, block, pool_w, forced, head_sum):
+    lens = [16, 63, 64, 65, 200, 511, 513, 1030]
+    say(f"select hq={hq} hkv={hkv} d={d} block={block} w={pool_w} forced={forced} sum={head_sum}")
+    c = filled(lens, hkv, d, block, 21)
+    check_select(c, hq, [32, 1, 7, 33, 32, 64, 5, 32], [max(forced, n // 3, 1) for n in lens], 22, pool_w, forced, head_sum)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (4, 4, 128)])
+def test_select_long_lists_ties_and_empty_sequences(hq, hkv, d):
+    """Lists around the limits of the ranking kernels, exact ties across the threshold, sequences without queries, rows or kept rows."""
+    lens = [4096, 4097, 8192, 8193, 0, 100, 1]
+    c = filled(lens, hkv, d, 32, 31, layout="head")
+    for b in (0, 2, 5):   # equal rows in the same block have equal codes and scales: equal scores
+        lo = int(c.cu[b])
+        for x in "kv":
+            c.t[x][lo + 64:lo + 96] = c.t[x][lo + 64]
+    torch.cuda.synchronize()
+    c.take()
+    check_select(c, hq, [32, 0, 8, 32, 3, 32, 1], [1500, 7, 8192, 4000, 0, 50, 1], 32)
+    check_select(c, hq, [32, 0, 8, 32, 3, 32, 1], [1500, 0, 2000, 4000, 0, 0, 1], 33, pool_w=3)
+
+
+def test_select_the_longest_list_and_many_sequences():
+    c = filled([32768, 5], 2, 64, 64, 41)
+    check_select(c, 2, [32, 32], [9000, 2], 42)
+    lens = [int(n) for n in np.random.default_rng(1).integers(1, 90, 150)]
+    c = filled(lens, 4, 64, 16, 43)
+    check_select(c, 16, [2] * 150, [max(1, n // 2) for n in lens], 44, pool_w=3)
+
+
+@pytest.mark.parametrize("hq,hkv,batch,n", [(16, 16, 16, 1024), (32, 8, 24, 2100), (32, 32, 9, 700)])
+def test_select_batches_that_take_one_launch_or_stream_k_once(hq, hkv, batch, n):
+    c = filled([n - 13 * b for b in range(batch)], hkv, 128, 32, 51)
+    check_select(c, hq, [32] * batch, [m // 5 for m in c.lens], 52)
+
+
+# ---------------------------------------------------------------- attention
+def reference_attention(c, q, cu_q, idx, cu_k, scale):
+    """(outputs, allowed error) in fp64."""
+    k, v = c.values("k"), c.values("v")
+    hq = q.shape[1]
+    g = hq // c.hkv
+    o, tol = np.zeros(q.shape), np.zeros(q.shape)
+    for b in range(len(cu_q) - 1):
+        q0, q1, n = int(cu_q[b]), int(cu_q[b + 1]), int(cu_k[b + 1] - cu_k[b])
+        if n == 0 or q1 == q0:
+            continue
+        for h in range(hq):
+            pos = int(c.cu[b]) + (np.arange(n) if idx is None else idx[h, int(cu_k[b]):int(cu_k[b + 1])])
+            kk, vv, qq = k[pos, h // g], v[pos, h // g], q[q0:q1, h]
+            z = qq @ kk.T * scale
+            size = np.abs(qq) @ np.abs(kk).T * scale
+            p = np.exp(z - z.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            out = p @ vv
+            # error factor of each p, times p |v - o|
+            d = 2.0 ** -8 / (1 - 2.0 ** -8) + (c.d + 2) * 2.0 ** -24 * size + 2.0 ** -21 + 2.0 ** -22 * np.abs(z) / math.log(2)
+            away = np.abs(vv[None, :, :] - out[:, None, :])
+            o[q0:q1, h] = out
+            tol[q0:q1, h] = (2 * np.einsum("qk,qkd->qd", p * (d - 2.0 ** -8), away) + 1.02 * 2.0 ** -8 * np.einsum("qk,qkd->qd", p, away)
+                             + 2.0 ** -8 * np.abs(out) + n * 2.0 ** -23 * (p @ np.abs(vv)) + 1e-30)
+    return o, tol
+
+
+def run_attend(c, q, cu_q, idx, cu_k, scale=None, stream=None):
+    scale = 1.0 / math.sqrt(c.d) if scale is None else scale
+    cu_qt, cu_kt = torch.from_numpy(cu_q).to(DEV), torch.from_numpy(cu_k).to(DEV)
+    max_q, max_k = int(np.diff(cu_q).max()), int(np.diff(cu_k).max())
+    batch = hcsa.make_cached_batch(q, cu_qt, c.cu_t, c.total, c.hkv, max_q, max(c.lens), scale)
+    o = torch.full((q.shape[0] + 1,) + tuple(q.shape[1:]), math.nan, dtype=torch.bfloat16, device=DEV)
+    it = None if idx is None else torch.from_numpy(np.ascontiguousarray(idx)).to(DEV)
+    hcsa.dllm_hcsa_attend_cached(batch, c.desc, it, cu_kt, int(cu_k[-1]), max_k, o[:-1])
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(o[-1]).all()), "wrote behind the last query"
+    return o[:-1]
+
+
+def check_attend(c, hq, qlens, keep, seed, lists=True, gain=1.0, q=None):
+    cu_q, cu_k = cu32(qlens), cu32(keep)
+    q = gain * normal(int(cu_q[-1]), hq, c.d, torch.bfloat16, seed) if q is None else q
+    rng = np.random.default_rng(seed)
+    idx = None
+    if lists:
+        idx = np.concatenate([np.stack([np.sort(rng.choice(n, m, replace=False)) for _ in range(hq)]) if m else np.zeros((hq, 0))
+                              for n, m in zip(c.lens, keep)], 1).astype(np.int32)
+    got = run_attend(c, q, cu_q, idx, cu_k).double().cpu().numpy()
+    want, tol = reference_attention(c, q.double().cpu().numpy(), cu_q, idx, cu_k, 1.0 / math.sqrt(c.d))
+    assert np.isfinite(got).all()
+    over = np.abs(got - want) - tol
+    assert over.max() <= 0, f"{int((over > 0).sum())} outputs off, by up to {np.abs(got - want)[over > 0].max():.3e}"
+    return idx
+
+
+HEADS = [(4, 4, 128, 32), (8, 2, 64, 16), (8, 1, 128, 64), (6, 2, 64, 32), (3, 3, 64, 64), (40, 8, 128, 16)]
+
+
+@pytest.mark.parametrize("lists", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,block", HEADS)
+def test_attention_over_ragged_sequences(hq, hkv, d, block, lists):
+    """Kept rows around tiles and chunks, query blocks around column tiles, nothing kept, no queries, one row."""
+    lens = [1, 40, 129, 300, 33, 700, 0, 64, 257]
+    keep = [1, 31, 129, 33, 0, 512, 0, 64, 97]
+    qlens = [1, 32, 33, 5, 4, 8, 2, 0, 70]
+    say(f"attend lists={lists} hq={hq} hkv={hkv} d={d} block={block}")
+    check_attend(filled(lens, hkv, d, block, 61), hq, qlens, keep, 62, lists)
+
+
+@pytest.mark.parametrize("lists", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,nq", [(8, 2, 128, 1), (2, 1, 64, 1), (16, 2, 64, 32), (1, 1, 128, 3)])
+def test_attention_of_few_heads_over_long_sequences(hq, hkv, d, nq, lists):
+    """Lists cut into many chunks, merged by a second launch; lengths that are no multiple of anything."""
+    lens = [5003, 2, 3000]
+    check_attend(filled(lens, hkv, d, 32, 71), hq, [nq] * 3, [4999, 1, 2111], 72, lists)
+
+
+@pytest.mark.parametrize("lists", [True, False])
+def test_attention_of_batches_above_64_sequences(lists):
+    lens = [int(n) for n in np.random.default_rng(2).integers(1, 200, 130)]
+    check_attend(filled(lens, 2, 64, 16, 81), 4, [1 + b % 3 for b in range(130)], [(n * 2 + 2) // 3 for n in lens], 82, lists)
+
+
+@pytest.mark.parametrize("lists", [True, False])
+def test_attention_of_more_lists_than_fit_at_once(lists):
+    lens = [int(n) for n in np.random.default_rng(3).integers(100, 400, 40)]
+    check_attend(filled(lens, 16, 64, 32, 83), 16, [16] * 40, [n // 2 for n in lens], 84, lists)
+
+
+@pytest.mark.parametrize("lists", [True, False])
+def test_large_scores_and_strided_queries(lists):
+    c = filled([400, 333], 2, 128, 32, 91, layout="padded")
+    wide = 8.0 * normal(40, 9, 136, torch.bfloat16, 92)
+    q = wide[:, :8, :128]
+    check_attend(c, 8, [32, 8], [200, 333], 93, lists, q=q)
+
+
+def test_unsorted_and_repeated_positions():
+    c = filled([50, 90], 2, 64, 16, 95)
+    q = normal(9, 4, 64, torch.bfloat16, 96)
+    idx = np.random.default_rng(4).integers(0, 50, (4, 120)).astype(np.int32)   # drawn with replacement: some count twice
+    cu_q, cu_k = cu32([4, 5]), cu32([48, 72])
+    got = run_attend(c, q, cu_q, idx, cu_k).double().cpu().numpy()
+    want, tol = reference_attention(c, q.double().cpu().numpy(), cu_q, idx, cu_k, 0.125)
+    assert (np.abs(got - want) <= tol).all()
+
+
+@pytest.mark.parametrize("lists", [True, False])
+def test_rows_that_nobody_attends_over_may_hold_anything(lists):
+    """NaN codes, NaN scales and the largest values in rows outside the lists, or behind the first k_b: not a bit changes."""
+    lens, keep, qlens = [200, 77, 64], [90, 33, 17], [32, 4, 1]
+    c = filled(lens, 2, 128, 32, 101)
+    idx = check_attend(c, 4, qlens, keep, 102, lists)
+    q = normal(37, 4, 128, torch.bfloat16, 102)
+    before = run_attend(c, q, cu32(qlens), idx, cu32(keep))
+    for b, (n, m) in enumerate(zip(lens, keep)):
+        lo = int(c.cu[b])
+        for g in range(2):
+            used = set(range(m)) if idx is None else {int(p) for h in (2 * g, 2 * g + 1) for p in idx[h, cu32(keep)[b]:cu32(keep)[b + 1]]}
+            free = [p for p in range(n) if p not in used]
+            for x in "kv":
+                c.t[x][[lo + p for p in free], g] = torch.tensor([127, 255, 126, 254], dtype=torch.uint8, device=DEV).repeat(32)
+                for blk in range(-(-n // 32)):
+                    if not any(p // 32 == blk for p in used):
+                        c.s[x][g, c.slot(b, 32 * blk)] = 255
+    torch.cuda.synchronize()
+    after = run_attend(c, q, cu32(qlens), idx, cu32(keep))
+    assert torch.equal(before.view(torch.int16), after.view(torch.int16))
+
+
+def test_a_nan_row_spoils_the_queries_that_attend_over_it_only():
+    lens, keep, qlens = [100, 60], [100, 60], [8, 8]
+    c = filled(lens, 2, 64, 32, 111)
+    q = normal(16, 4, 64, torch.bfloat16, 112)
+    before = run_attend(c, q, cu32(qlens), None, cu32(keep))
+    c.t["k"][50, 1, 5] = 127
+    torch.cuda.synchronize()
+    after = run_attend(c, q, cu32(qlens), None, cu32(keep))
+    assert bool(torch.isnan(after[:8, 2:]).all())
+    assert torch.equal(before[:8, :2], after[:8, :2]) and torch.equal(before[8:], after[8:])
+    assert bool(torch.isfinite(after[:8, :2]).all())
+
+
+def test_offsets_beyond_32_bits():
+    """A cache that spans 6 GB, of sequences of less than 4 GiB each: every call on its last rows."""
+    pitch, lens = 1 << 20, [3000, 3100]
+    total, hkv, d = sum(lens), 2, 128
+    base = {x: torch.zeros(total * pitch, dtype=torch.uint8, device=DEV) for x in "kv"}
+    c = Cache(lens, hkv, d, 32)
+    c.t = {x: base[x].as_strided((total, hkv, d), (pitch, 128, 1), 0) for x in "kv"}
+    c.desc = hcsa.make_cache(c.t["k"], c.t["v"], c.s["k"], c.s["v"], 32)
+    c.write(normal(total, hkv, d, torch.bfloat16, 121), normal(total, hkv, d, torch.bfloat16, 122))
+    c.check()
+    k, v = read_back(c)
+    torch.cuda.synchronize()
+    assert np.array_equal(k.double().cpu().numpy(), c.values("k")) and np.array_equal(v.double().cpu().numpy(), c.values("v"))
+    check_select(c, 4, [32, 32], [100, 900], 123)
+    check_attend(c, 4, [32, 1], [150, 1200], 124)
+    check_attend(c, 4, [1, 2], [2990, 3100], 125, lists=False)
+
+
+# ---------------------------------------------------------------- together
+def test_a_denoising_step_on_the_cache():
+    """The block's rows go to the end of every sequence, the kept positions always hold them, the block attends."""
+    lens, hkv, hq, d, n = [300, 161, 97], 2, 8, 128, 32
+    c = filled(lens, hkv, d, 32, 131)
+    for turn in range(3):
+        rows = [normal(3 * n, hkv, d, torch.bfloat16, 132 + 10 * turn + i, 0.05) * (1 + 3 * turn) for i in range(2)]
+        c.write(*rows, [m - n for m in lens], [n] * 3)
+        c.check()
+        q = normal(3 * n, hq, d, torch.bfloat16, 140 + turn)
+        keep = [100, 80, 32]
+        idx = check_select(c, hq, [n] * 3, keep, 0, pool_w=3, forced=n, q=q)
+        got = run_attend(c, q, cu32([n] * 3), idx, cu32(keep)).double().cpu().numpy()
+        want, tol = reference_attention(c, q.double().cpu().numpy(), cu32([n] * 3), idx, cu32(keep), 1 / math.sqrt(d))
+        assert (np.abs(got - want) <= tol).all()
+
+
+def test_decoding_token_by_token():
+    """Sequences with room for 90 tokens grow by one token a step; places that are not filled yet hold zeros."""
+    hkv, hq, d, room = 2, 8, 64, [90, 70, 75]
+    c = Cache(room, hkv, d, 16)
+    have = [1, 40, 15]
+    first = [normal(sum(have), hkv, d, torch.bfloat16, 151 + i) for i in range(2)]
+    c.write(*first, [0, 0, 0], have)
+    for step in range(20):
+        new = [normal(3, hkv, d, torch.bfloat16, 160 + 2 * step + i) * (1.0 + step % 5) for i in range(2)]
+        c.write(*new, have, [1, 1, 1])
+        have = [n + 1 for n in have]
+        if step % 4 == 3:
+            c.check()
+            check_attend(c, hq, [1, 1, 1], have, 200 + step, lists=False)
+
+
+def test_calls_are_the_same_every_time_and_on_another_stream():
+    lens, keep, qlens = [900, 411, 1200], [800, 400, 70], [32, 1, 32]
+    c = filled(lens, 2, 128, 32, 171)
+    q = normal(65, 8, 128, torch.bfloat16, 172)
+    for idx in (check_attend(c, 8, qlens, keep, 173), None):
+        one = run_attend(c, q, cu32(qlens), idx, cu32(keep))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            two = run_attend(c, q, cu32(qlens), idx, cu32(keep))
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(one.view(torch.int16), two.view(torch.int16))
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_a_step_replayed_from_a_hip_graph(decode):
+    """Two graphs that share their workspaces, replayed in turn with new rows, queries and places, beside eager work; every
+    replay against the eager calls on a copy of the cache."""
+    lens, hkv, hq, d, n = [1500, 700], 2, 8, 128, (1 if decode else 32)
+    dev = torch.device(DEV)
+    c, e = filled(lens, hkv, d, 32, 181), filled(lens, hkv, d, 32, 181)
+    cu_q = torch.tensor([0, n, 2 * n], dtype=torch.int32, device=dev)
+    cu_rows, at = cu_q.clone(), torch.tensor([m - n for m in lens], dtype=torch.int32, device=dev)
+    keep = [1000, 600]
+    cu_k = torch.tensor(cu32(keep), device=dev)
+    k, v = torch.zeros((2 * n, hkv, d), dtype=torch.bfloat16, device=dev), torch.zeros((2 * n, hkv, d), dtype=torch.bfloat16, device=dev)
+    q = torch.zeros((2 * n, hq, d), dtype=torch.bfloat16, device=dev)
+    idx = torch.zeros((hq, sum(keep)), dtype=torch.int32, device=dev)
+    batch = hcsa.make_cached_batch(q, cu_q, c.cu_t, c.total, hkv, n, max(lens), 0.09)
+    rows = hcsa.make_rows_batch(k, v, c.cu_t, c.total, max(lens))
+    space = {x: torch.empty(max(1, f(batch, c.desc, max(keep))), dtype=torch.uint8, device=dev)
+             for x, f in (("s", hcsa.dllm_hcsa_select_cached_workspace), ("a", hcsa.dllm_hcsa_attend_cached_workspace))}
+
+    def step(cache, o, ws):
+        hcsa.dllm_hcsa_cache_write(rows, cache, cu_rows, 2 * n, n, at)
+        if not decode:
+            hcsa.dllm_hcsa_select_cached(batch, cache, cu_k, sum(keep), max(keep), idx, 3, 0, False, ws["s"] if ws else None)
+        hcsa.dllm_hcsa_attend_cached(batch, cache, None if decode else idx, cu_k, sum(keep), max(keep), o, ws["a"] if ws else None)
+
+    graphs, outs = [], []
+    warm = torch.cuda.Stream()
+    warm.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(warm):
+        step(c.desc, torch.empty_like(q), space)
+        step(e.desc, torch.empty_like(q), space)
+    torch.cuda.current_stream().wait_stream(warm)
+    for _ in range(2):
+        o, graph = torch.empty_like(q), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(c.desc, o, space)
+        graphs.append(graph)
+        outs.append(o)
+    for turn in range(6):
+        k.copy_(normal(2 * n, hkv, d, torch.bfloat16, 190 + turn) * (1 + turn))
+        v.copy_(normal(2 * n, hkv, d, torch.bfloat16, 290 + turn))
+        q.copy_(normal(2 * n, hq, d, torch.bfloat16, 390 + turn))
+        at.copy_(torch.tensor([(137 * turn) % (lens[0] - n + 1), (91 * turn) % (lens[1] - n + 1)], dtype=torch.int32))
+        graphs[turn % 2].replay()
+        torch.cuda.synchronize()
+        torch.randn(1000, device=dev).sum()
+        got = idx.clone()
+        want = torch.empty_like(q)
+        step(e.desc, want, None)
+        torch.cuda.synchronize()
+        assert torch.equal(got, idx)
+        assert torch.equal(outs[turn % 2].view(torch.int16), want.view(torch.int16)) and bool(torch.isfinite(want).all())
+        for x in "kv":
+            assert torch.equal(c.t[x], e.t[x]) and torch.equal(c.s[x], e.s[x])
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_shapes_through_every_call(seed):
+    rng = np.random.default_rng(1000 + seed)
+    d, block = int(rng.choice([64, 128])), int(rng.choice([16, 32, 64]))
+    hkv, group, batch = int(rng.integers(1, 6)), int(rng.integers(1, 6)), int(rng.integers(1, 10))
+    lens = [int(rng.integers(1, 500)) for _ in range(batch)]
+    keep = [int(rng.integers(1, n + 1)) for n in lens]
+    qlens = [int(rng.integers(1, 50)) for _ in range(batch)]
+    say(f"random {seed}: d={d} block={block} hkv={hkv} group={group} lens={lens} keep={keep} q={qlens}")
+    c = Cache(lens, hkv, d, block, str(rng.choice(["token", "head", "padded"])))
+    dtype = torch.bfloat16 if seed % 3 else torch.float32
+    c.write(normal(c.total, hkv, d, dtype, seed), normal(c.total, hkv, d, dtype, seed + 50))
+    counts = [int(rng.integers(0, n + 1)) for n in lens]
+    starts = [int(rng.integers(0, n - m + 1)) for n, m in zip(lens, counts)]
+    if sum(counts):
+        c.write(5 * normal(sum(counts), hkv, d, dtype, seed + 60), normal(sum(counts), hkv, d, dtype, seed + 70), starts, counts)
+    c.check()
+    check_select(c, hkv * group, qlens, keep, seed, pool_w=int(rng.choice([1, 3])))
+    check_attend(c, hkv * group, qlens, keep, seed, True)
+    check_attend(c, hkv * group, qlens, keep, seed, False)
+
+
+# ---------------------------------------------------------------- the checked build
+def test_checked_library_reports_bad_offsets_and_writes_nothing():
+    hcsa.use_checked_library(True)
+    try:
+        c = filled([64, 40], 2, 64, 32, 221)
+        before = {x: c.t[x].clone() for x in "kv"}
+        assert hcsa.dllm_hcsa_precondition_errors() == 0
+        k = normal(104, 2, 64, torch.bfloat16, 222)
+        for cu, total, most, bit in (([0, 30, 71], 71, 41, hcsa.DLLM_CHECK_K_OVER_L), ([0, 30, 20], 40, 40, hcsa.DLLM_CHECK_CU_K),
+                                     ([1, 30, 40], 40, 40, hcsa.DLLM_CHECK_CU_K)):
+            batch = hcsa.make_rows_batch(k, k, c.cu_t, c.total, 64)
+            hcsa.dllm_hcsa_cache_write(batch, c.desc, torch.tensor(cu, dtype=torch.int32, device=DEV), total, most)
+            assert hcsa.dllm_hcsa_precondition_errors() & bit, cu
+            out = [torch.full_like(k, 7.0) for _ in "kv"]
+            batch = hcsa.make_rows_batch(*out, c.cu_t, c.total, 64)
+            hcsa.dllm_hcsa_cache_read(batch, c.desc, *out, torch.tensor(cu, dtype=torch.int32, device=DEV), total, most)
+            assert hcsa.dllm_hcsa_precondition_errors() & bit
+            assert bool((out[0] == 7).all()) and all(torch.equal(before[x], c.t[x]) for x in "kv")
+        q = normal(8, 4, 64, torch.bfloat16, 223)
+        cu_q, cu_k = torch.tensor([0, 4, 8], dtype=torch.int32, device=DEV), torch.tensor([0, 20, 30], dtype=torch.int32, device=DEV)
+        batch = hcsa.make_cached_batch(q, cu_q, c.cu_t, c.total, 2, 4, 64, 0.125)
+        idx = torch.zeros((4, 30), dtype=torch.int32, device=DEV)
+        o = torch.full_like(q, 7.0)
+        idx[1, 25] = 40   # the second sequence has rows 0 .. 39
+        hcsa.dllm_hcsa_attend_cached(batch, c.desc, idx, cu_k, 30, 20, o)
+        assert hcsa.dllm_hcsa_precondition_errors() == hcsa.DLLM_CHECK_IDX and bool((o == 7).all())
+        idx[1, 25] = 39
+        hcsa.dllm_hcsa_attend_cached(batch, c.desc, idx, cu_k, 30, 20, o)
+        assert hcsa.dllm_hcsa_precondition_errors() == 0 and not bool((o == 7).any())
+        bad = torch.tensor([0, 20, 61], dtype=torch.int32, device=DEV)
+        idx2 = torch.full((4, 61), -3, dtype=torch.int32, device=DEV)
+        hcsa.dllm_hcsa_select_cached(batch, c.desc, bad, 61, 41, idx2)
+        assert hcsa.dllm_hcsa_precondition_errors() & hcsa.DLLM_CHECK_K_OVER_L and bool((idx2 == -3).all())
+    finally:
+        hcsa.use_checked_library(False)
