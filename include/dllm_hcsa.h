@@ -336,9 +336,16 @@ dllm_status dllm_hcsa_select_cached(const dllm_batch *batch, const dllm_cache *c
  * autoregressive model (cu_kv gives every sequence's room, cu_k how much of it is filled) or a block over everything.  A
  * sequence with k_b == 0 gets zeros.  A query whose scores are NaN or overflow to plus infinity, or that attends over a NaN,
  * gets NaN; no other query's output changes.  A row that no query attends over may hold anything.
- * The workspace query takes idx or no idx alike.
+ * The workspace query serves calls with and without idx.
  */
 size_t dllm_hcsa_attend_cached_workspace(const dllm_batch *batch, const dllm_cache *cache, int32_t max_k);
+/*
+ * How a call shares out its work, for tests and measurement: 0 if every list goes to a workgroup of its own, else the rows per piece
+ * in which the lists, laid end to end, are cut (lists that a cut goes through are merged by a second launch); -1 if the arguments
+ * are invalid.  lists: 1 for a call with idx, 0 for one without.  Host only: no device memory is read, nothing launched.
+ */
+int32_t dllm_hcsa_attend_cached_form_of(const dllm_batch *batch, const dllm_cache *cache, int32_t lists, int32_t max_k,
+                                        int32_t total_k);
 dllm_status dllm_hcsa_attend_cached(const dllm_batch *batch, const dllm_cache *cache,
                                     const int32_t *idx,  /* device, [n_q_heads, total_k], or NULL */
                                     const int32_t *cu_k, /* device, [batch+1] */

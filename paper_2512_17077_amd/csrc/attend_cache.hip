@@ -22,7 +22,7 @@
 namespace dllm {
 
 constexpr int kWaves = 4;
-constexpr int kMaxChunkRows = 2048;   // kept rows of a list that one workgroup walks at most (their ids lie in LDS)
+constexpr int kMaxListRows = 2048;   // kept rows of a list that one workgroup walks at most (their ids lie in LDS)
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf2;
 
@@ -38,295 +38,549 @@ __device__ __forceinline__ void widen_codes(v4u x, float unit, v4u& lo, v4u& hi)
   hi = v4u{y[4], y[5], y[6], y[7]};
 }
 
-// QG: a sequence's column tiles are shared out to several workgroups (blockIdx.z counts sequences, then groups of tiles)
-template <int D, bool Lists, bool QG>
+// Order of a row's 16-byte chunks of bf16 in an LDS tile: a lane converts 16 codes into two of them, and lays them half a row
+// apart, so that lanes side by side write chunks side by side (next to each other they would use every other bank only).  The queries
+// have the same order, so the sums over head_dim do not notice; outputs take it back.
+template <int D>
+__device__ __forceinline__ int place(int chunk) { return (chunk >> 1) + (chunk & 1) * (D / 16); }
+template <int D>
+__device__ __forceinline__ int placed(int at) { return at < D / 16 ? 2 * at : 2 * (at - D / 16) + 1; }
+
+// Byte offset of 16-byte chunk `cc` of `row` in a tile of codes, permuted so that lanes with neighbouring rows read one
+// chunk of each from different banks.
+template <int D>
+__device__ __forceinline__ int codes_off(int row, int cc) {
+  return row * D + ((cc ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4);
+}
+
+// What a workgroup takes of one sequence: rows c0 .. c1-1 of its list, one of `parts` segments of it.
+struct Segment {
+  int b, k0, kb, c0, c1, parts, q0, nq, kv0;
+};
+
+// sequence that list position r belongs to: the last one with cu_k[b] <= r among those that keep something
+__device__ __forceinline__ int sequence_at(const int32_t* __restrict__ cu_k, int batch, int r, int lane) {
+  int lo = 0, n = batch;   // it lies in lo .. lo+n-1
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const bool below = lane * step < n && cu_k[lo + lane * step] <= r;
+    const int at = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(below) | 1ull);   // cu_k does not decrease
+    lo += at * step;
+    n = min(step, n - at * step);
+  }
+  return lo;
+}
+
+// Order in which lists that are taken whole are started.  Two workgroups are resident per compute unit, and workgroup i shares its
+// unit with workgroup i + 256 (measured: see below), so where all lists are resident but not one per unit, the longest are
+// left alone and the others folded, shortest with longest: with pairs = lists beyond 256, the first `pairs` places go to the
+// shortest, in rising order, the next to the longest, and those that come second are in falling order.  32 heads x 128, lists of 5 to 50 % of 512 to
+// 4096 positions, mean over six draws, as they come / longest first / folded: 9 sequences 18.2 / 19.5 / 17.4 us, 12 24.6 / 23.6 / 20.4, 14
+// 27.8 / 26.1 / 22.1, 16 28.9 / 27.7 / 25.2.  With more lists than are resident, longest first: 20 sequences 35.8 / 32.3.
+enum : int { kAsTheyCome = 0, kLongestFirst = 1, kFolded = 2 };
+constexpr int kUnits = 256;   // compute units
+
+// Rows are shared out in pieces (Pieces): the lists of one head, laid end to end as cu_k has them, are cut every `piece` rows, and
+// a workgroup takes one piece of one head, whatever sequences it holds.  So all workgroups have the same work however long
+// the lists are, and those that a cut goes through are merged by a second launch.  Otherwise a workgroup takes one list whole.
+template <int D, bool Lists, bool Pieces>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
     const uint16_t* __restrict__ q, CacheView c, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_kv,
     const int32_t* __restrict__ idx, const int32_t* __restrict__ cu_k, int32_t total_k, uint16_t* __restrict__ o,
-    float* __restrict__ po, float* __restrict__ pm, float* __restrict__ pl, int32_t chunk_rows, int ranked,
+    float* __restrict__ po, float2* __restrict__ pml, int32_t piece, int order,
     Shape s DLLM_CHECK_PARAM) {
   DLLM_CHECK_EXIT();
-  constexpr int CH = D / 8;             // 16-byte chunks of a bf16 row
-  constexpr int CC = D / 16;            // ... of a row of codes
-  constexpr int TILEB = kTile * 2 * D;
+  constexpr int CC = D / 16;            // 16-byte chunks of a row of codes
+  constexpr int KTILEB = kTile * D, VTILEB = kTile * 2 * D;   // K lies in LDS as codes, V as bf16
   constexpr int NLD = kTile * CC / 64;  // 16-byte loads per lane, tile and tensor
   constexpr int NDB = D / 32;
+  constexpr int NT = D / 16;            // matrix-core steps along head_dim
   constexpr int W = kWaves;
-  constexpr int MAXT = kMaxChunkRows / (W * kTile);
-  constexpr int kDepth = D == 128 ? 2 : 4;   // tiles in flight per wave
+  constexpr int MAXT = kMaxListRows / kTile / W;
+  constexpr int kDepth = D == 128 ? 1 : 2;   // tiles in flight per wave
   constexpr int kMl = Lists ? MAXT * kTile : 64;
 
-  __shared__ __attribute__((aligned(16))) char lds[W][2 * TILEB];   // per wave: K tile, V tile; merge space afterwards
-  __shared__ __attribute__((aligned(16))) char qtile[TILEB];
+  constexpr int WAVEB = KTILEB + VTILEB > NDB * 4096 ? KTILEB + VTILEB : NDB * 4096;
+  __shared__ __attribute__((aligned(16))) char lds[W][WAVEB];   // per wave: K tile, V tile; its accumulators at the merge
   __shared__ int sm_rows[W][kMl];   // kept-row ids of each wave's tiles; (m, l) at the merge
 
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int col = lane & 31, hf = lane >> 5;
-  const int chunk = blockIdx.x;
-  int slot = blockIdx.z, qt0 = 0, qstep = 1;
-  if constexpr (QG) {
-    qt0 = slot / s.batch;
-    slot -= qt0 * s.batch;
-    qstep = int(gridDim.z) / s.batch;
+  constexpr bool kHeadsFirst = Lists || !Pieces;
+  int unit = kHeadsFirst ? blockIdx.x : blockIdx.y, px = kHeadsFirst ? blockIdx.y : blockIdx.x;
+  if constexpr (kHeadsFirst && D == 64) {
+    // Rows of 64 bytes: two heads share a 128-byte line, so they go to one XCD and its L2 (workgroup i runs on XCD i % 8): of sixteen
+    // workgroups in a row, the second eight take the other heads of the first eight's pairs.
+    const uint32_t n = gridDim.x, at = blockIdx.x + n * blockIdx.y;
+    if (n % 2 == 0 && (at | 15u) < n * gridDim.y) {
+      const uint32_t pair = at / 16 * 8 + at % 8;
+      px = int(pair / (n / 2));
+      unit = int(2 * (pair % (n / 2)) + at / 8 % 2);
+    }
   }
-  const SeqInfo si = sequence_of_slot(cu_q, cu_kv, cu_k, s.batch, slot, lane, ranked != 0);
-  const int kb = si.kb, q0 = si.q0, nq = si.nq, kv0 = si.kv0;
-  const ChunkGeom cg = chunk_geom(kb, chunk_rows);
-  const int c0 = chunk * cg.rows;
-  if (c0 >= kb && !(chunk == 0 && kb == 0)) return;
-  const int c1 = min(kb, c0 + cg.rows);
-  const int h0 = Lists ? int(blockIdx.y) : int(blockIdx.y) * s.group;   // first query head
-  const int g = Lists ? h0 / s.group : int(blockIdx.y);
+  const int h0 = Lists ? unit : unit * s.group;   // first query head
+  const int g = Lists ? h0 / s.group : unit;
   const int heads = Lists ? 1 : s.group;
-  const int ncols = nq * heads;
-  if (qt0 * 32 >= ncols) return;
-  // column x of this workgroup: query x / heads, head h0 + x % heads
+  // column x of a sequence: query x / heads, head h0 + x % heads
   auto query_of = [&](int x) { return Lists ? x : int(uint32_t(x) / uint32_t(heads)); };
-  if (kb == 0) {   // nothing kept: defined as zeros
-    if (qt0 == 0)
-      for (int e = threadIdx.x; e < ncols * D; e += W * 64) {
-        const int x = e / D, i = query_of(x);
-        o[(int64_t(q0 + i) * s.hq + h0 + (x - i * heads)) * D + e % D] = 0;
-      }
-    return;
+  auto clear = [&](int q0, int nq) {   // nothing kept: defined as zeros
+    for (int e = threadIdx.x; e < nq * heads * D; e += W * 64) {
+      const int x = e / D, i = query_of(x);
+      o[(int64_t(q0 + i) * s.hq + h0 + (x - i * heads)) * D + e % D] = 0;
+    }
+  };
+
+  Segment sg;
+  int end = 0;   // list position behind this piece
+  [[maybe_unused]] BatchInfo bi;
+  [[maybe_unused]] const bool small = s.batch <= kRankBatch;   // (lane i holds sequence i's offsets)
+  // the first sequence from b on that keeps something, and what of it lies in this piece
+  auto enter = [&](int b) {
+    if (small) {
+      const uint64_t some = __builtin_amdgcn_ballot_w64(lane < s.batch && lane >= b && bi.kb > 0);
+      b = some ? __builtin_ctzll(some) : s.batch - 1;
+      sg.k0 = __builtin_amdgcn_readlane(bi.ko0, b);
+      sg.kb = __builtin_amdgcn_readlane(bi.kb, b);
+      sg.q0 = __builtin_amdgcn_readlane(bi.q0, b);
+      sg.nq = __builtin_amdgcn_readlane(bi.nq, b);
+      sg.kv0 = __builtin_amdgcn_readlane(bi.kv0, b);
+    } else {
+      while (b < s.batch - 1 && cu_k[b + 1] == cu_k[b]) ++b;
+      sg.k0 = cu_k[b];
+      sg.kb = cu_k[b + 1] - sg.k0;
+      sg.q0 = cu_q[b];
+      sg.nq = cu_q[b + 1] - sg.q0;
+      sg.kv0 = cu_kv[b];
+    }
+    const int k1 = sg.k0 + sg.kb, fp = int(uint32_t(sg.k0) / uint32_t(piece));
+    sg.b = b;
+    sg.c0 = max(px * piece, sg.k0) - sg.k0;
+    sg.c1 = min(end, k1) - sg.k0;
+    sg.parts = sg.kb > 0 ? int(uint32_t(k1 - 1) / uint32_t(piece)) - fp + 1 : 1;
+  };
+  if constexpr (Pieces) {
+    const int first = int(min(int64_t(px) * piece, int64_t(INT32_MAX)));   // (the grid may have a few more than there are pieces)
+    int b = 0;
+    if (small) {
+      bi = load_batch(cu_q, cu_kv, cu_k, s.batch, lane, false);
+      end = __builtin_amdgcn_readlane(bi.ko0 + bi.kb, s.batch - 1);
+      const uint64_t behind = __builtin_amdgcn_ballot_w64(lane < s.batch && bi.ko0 + bi.kb > first);
+      b = behind ? __builtin_ctzll(behind) : 0;
+    } else {
+      end = cu_k[s.batch];
+      b = sequence_at(cu_k, s.batch, first, lane);
+    }
+    if (px == 0 && blockIdx.z == 0)
+      for (int i = 0; i < s.batch; ++i)
+        if (cu_k[i + 1] == cu_k[i]) clear(cu_q[i], cu_q[i + 1] - cu_q[i]);
+    if (first >= end) return;
+    end = int(min(int64_t(first) + piece, int64_t(end)));
+    enter(b);
+  } else {
+    int place_of = px;
+    if (order == kFolded) {
+      const int first_round = (kUnits + int(gridDim.x) - 1) / int(gridDim.x), pairs = s.batch - first_round;
+      place_of = px < pairs ? s.batch - 1 - px : px - pairs;
+    }
+    const SeqInfo si = sequence_of_slot(cu_q, cu_kv, cu_k, s.batch, place_of, lane, order != kAsTheyCome);
+    if (si.kb == 0) {
+      if (blockIdx.z == 0) clear(si.q0, si.nq);
+      return;
+    }
+    sg = {si.b, si.ko0, si.kb, 0, Lists ? min(si.kb, kMaxListRows) : si.kb, 1, si.q0, si.nq, si.kv0};
   }
 
-  const int32_t* __restrict__ rows = idx + int64_t(h0) * total_k + si.ko0;
-  const uint8_t* kbase = c.k + int64_t(kv0) * c.tok + int64_t(g) * c.head;
-  const uint8_t* vbase = c.v + int64_t(kv0) * c.tok + int64_t(g) * c.head;
-  const int64_t scale0 = g * c.scale_head + scale_slot(kv0, si.b, c.shift);
-  const uint8_t* sbase = (hf == 0 ? c.ks : c.vs) + scale0;
-  const uint32_t pitch = uint32_t(c.tok);   // a sequence's rows span < 4 GiB (checked on the host)
-  const float zscale = s.scale * kLog2e;
-  const int ntiles = (c1 - c0 + kTile - 1) / kTile;
   char* ktile = lds[wave];
-  char* vtile = lds[wave] + TILEB;
-  KAddr<D> ka;
-  ka.init(lane);
+  char* vtile = lds[wave] + KTILEB;
+  const int koff = codes_off<D>(col, hf);   // K operand: chunks 2u + hf of row col
   VtAddr<D> vt;
   vt.init(lane);
-  const uint32_t coff = (lane % CC) * 16;
+  const uint32_t coff = uint32_t(lane) % CC * 16;
+  const uint32_t pitch = uint32_t(c.tok);   // a sequence's rows span < 4 GiB (checked on the host)
+  const float zscale = s.scale * kLog2e;
   auto opaque = [](int x) {
     asm volatile("" : "+v"(x));
     return x;
   };
 
-  for (int qt = qt0; qt * 32 < ncols; qt += qstep) {
-    float m_used = -FLT_MAX, lsum = 0.0f;
-    f32x16 acc[NDB];
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[db][i] = 0.0f;
+  for (;;) {   // segments of the piece
+    const int ncols = sg.nq * heads;
+    const uint8_t* kbase = c.k + int64_t(sg.kv0) * c.tok + int64_t(g) * c.head;
+    const uint8_t* vbase = c.v + int64_t(sg.kv0) * c.tok + int64_t(g) * c.head;
+    const uint8_t* sbase = (hf == 0 ? c.ks : c.vs) + g * c.scale_head + scale_slot(sg.kv0, sg.b, c.shift);
+    const int32_t* __restrict__ rows = idx + int64_t(h0) * total_k + sg.k0;
+    const int c0 = sg.c0, c1 = sg.c1;
+    const int ntiles = c1 > c0 ? (c1 - c0 + kTile - 1) / kTile : 0;
+    // a wave's tiles are neighbours: it walks a span of its own
+    const int t0 = ntiles * wave / W, mine = ntiles * (wave + 1) / W - t0;
 
-    int* my_rows = sm_rows[wave];
-    if constexpr (Lists) {   // ids of this wave's tiles (positions past the end repeat the last row, which is masked)
+    for (int qt = blockIdx.z; ntiles > 0 && qt * 32 < ncols; qt += gridDim.z) {
+      float m_used = -FLT_MAX, lsum = 0.0f;
+      f32x16 acc[NDB];
 #pragma unroll
-      for (int jj = 0; jj < MAXT / 2; ++jj) {
-        const int p = jj * 64 + lane;
-        const int t = min(c0 + (wave + (p >> 5) * W) * kTile + (p & 31), c1 - 1);
-        my_rows[p] = rows[t];
-      }
-    }
-    constexpr int NQL = (kTile * CH + W * 64 - 1) / (W * 64);
-    v4u qx[NQL];
+      for (int db = 0; db < NDB; ++db)
 #pragma unroll
-    for (int i = 0; i < NQL; ++i) {
-      const int f = i * W * 64 + threadIdx.x, r = f / CH, x = qt * 32 + r;
-      qx[i] = v4u{0u, 0u, 0u, 0u};
-      if (r < kTile && x < ncols) {
-        const int qi = query_of(x);
-        qx[i] = *reinterpret_cast<const v4u*>(q + int64_t(q0 + qi) * s.q_tok + int64_t(h0 + (x - qi * heads)) * s.q_head +
-                                              (f % CH) * 8);
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (int i = 0; i < 16; ++i) acc[db][i] = 0.0f;
 
-    v4u kr[kDepth][NLD], vr[kDepth][NLD];
-    uint32_t sc[kDepth];
-    // row `r` (0 .. 31) of the wave's j-th tile
-    auto row_of = [&](int j, int r) {
-      return Lists ? my_rows[j * kTile + r] : min(c0 + (wave + j * W) * kTile + r, c1 - 1);
-    };
-    auto fetch = [&](v4u (&kx)[NLD], v4u (&vx)[NLD], uint32_t& sx, int j) {
-      sx = sbase[uint32_t(row_of(j, col)) >> c.shift];
+      int* my_rows = sm_rows[wave];
+      if constexpr (Lists) {   // ids of this wave's tiles (positions past the end repeat the last row, which is masked)
 #pragma unroll
-      for (int i = 0; i < NLD; ++i) {
-        const uint32_t off = __umul24(uint32_t(row_of(j, (i * 64 + lane) / CC)), pitch) + coff;
-        kx[i] = load_once(kbase + off);
-        vx[i] = load_once(vbase + off);
-      }
-    };
-#pragma unroll
-    for (int d = 0; d < kDepth; ++d)
-      if (wave + d * W < ntiles) fetch(kr[d], vr[d], sc[d], d);
-#pragma unroll
-    for (int i = 0; i < NQL; ++i) {
-      const int f = i * W * 64 + threadIdx.x, r = f / CH;
-      if (r < kTile) *reinterpret_cast<v4u*>(qtile + tile_off<D>(r, f % CH)) = qx[i];
-    }
-    __syncthreads();   // the queries are in place
-    for (int j0 = 0; wave + j0 * W < ntiles; j0 += kDepth) {
-#pragma unroll
-      for (int d = 0; d < kDepth; ++d) {
-        const int j = j0 + d, tile = wave + j * W;
-        if (tile < ntiles) {
-          KAddr<D> kar;
-          kar.base = opaque(ka.base);
-          VtAddr<D> vtr;
-          vtr.base[0] = opaque(vt.base[0]);
-          vtr.base[1] = opaque(vt.base[1]);
-          const int lane_o = opaque(lane);
-#pragma unroll
-          for (int i = 0; i < NLD; ++i) {
-            const int f = i * 64 + lane_o, r = f / CC, cc = f % CC;
-            const float ku = scale_of(uint32_t(__builtin_amdgcn_ds_bpermute(r * 4, int(sc[d]))));
-            const float vu = scale_of(uint32_t(__builtin_amdgcn_ds_bpermute(r * 4 + 128, int(sc[d]))));
-            v4u lo, hi;
-            widen_codes(kr[d][i], ku, lo, hi);
-            *reinterpret_cast<v4u*>(ktile + tile_off<D>(r, 2 * cc)) = lo;
-            *reinterpret_cast<v4u*>(ktile + tile_off<D>(r, 2 * cc + 1)) = hi;
-            widen_codes(vr[d][i], vu, lo, hi);
-            *reinterpret_cast<v4u*>(vtile + tile_off<D>(r, 2 * cc)) = lo;
-            *reinterpret_cast<v4u*>(vtile + tile_off<D>(r, 2 * cc + 1)) = hi;
-          }
-          if (tile + kDepth * W < ntiles) fetch(kr[d], vr[d], sc[d], j + kDepth);
-          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-          sparse_tile_math<D>(ktile, vtile, qtile, kar, vtr, hf, c1 - (c0 + tile * kTile), zscale, m_used, lsum, acc);
-          __builtin_amdgcn_wave_barrier();
+        for (int jj = 0; jj < MAXT / 2; ++jj) {
+          const int p = jj * 64 + lane;
+          const int t = min(c0 + (t0 + (p >> 5)) * kTile + (p & 31), c1 - 1);
+          my_rows[p] = rows[t];
         }
       }
-    }
-
-    // ---- merge the waves' (m, l, O^T) through LDS that only they have used (as in attend_sparse_bf16_kernel)
-    const float l = sum_across_halves(lsum);
-    float* sm_ml = reinterpret_cast<float*>(&sm_rows[0][0]);   // [wave][m: 32 | l: 32], row stride kMl
-    if (hf == 0) {
-      sm_ml[wave * kMl + col] = m_used;
-      sm_ml[wave * kMl + 32 + col] = l;
-    }
-    float4* mrg = reinterpret_cast<float4*>(&lds[0][0]);
-    constexpr int kMrgWave = 2 * TILEB / 16;
-    static_assert(NDB * 4 * 64 <= kMrgWave, "a wave's accumulators fit its tile buffers");
+      // The queries stay in registers: this lane's column, in the order in which the lane's half of a K row comes (operand t of the
+      // products: elements 16 * (t - t % 2 + hf) + 8 * (t % 2) ..)
+      v4u qx[NT];
+      {
+        const int x = min(qt * 32 + col, ncols - 1);   // past the last column: that one again, never stored
+        const int qi = query_of(x);
+        const uint16_t* qp = q + int64_t(sg.q0 + qi) * s.q_tok + int64_t(h0 + (x - qi * heads)) * s.q_head + 16 * hf;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4)
-        mrg[wave * kMrgWave + (db * 4 + i4) * 64 + lane] =
-            make_float4(acc[db][4 * i4 + 0], acc[db][4 * i4 + 1], acc[db][4 * i4 + 2], acc[db][4 * i4 + 3]);
-    __syncthreads();
-    {
-      constexpr int PARTS = W / NDB, NQ4 = 4 / PARTS;
-      static_assert(W % NDB == 0 && 4 % PARTS == 0, "the waves split the output evenly");
-      const int db = wave % NDB, i4_0 = (wave / NDB) * NQ4;
-      float m_all = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < W; ++w) m_all = fmaxf(m_all, sm_ml[w * kMl + col]);
-      float f[W];
-      float l_all = 0.0f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(sm_ml[w * kMl + col] - m_all);   // 0 for a wave that saw no tile
-        l_all += sm_ml[w * kMl + 32 + col] * f[w];
+        for (int t = 0; t < NT; ++t) qx[t] = *reinterpret_cast<const v4u*>(qp + 16 * (t & ~1) + 8 * (t & 1));
       }
-      const int x = qt * 32 + col;
-      const int qi = query_of(x);
-      const int64_t row = int64_t(q0 + qi) * s.hq + h0 + (x - qi * heads);
-      const float inv = 1.0f / l_all;
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+
+      v4u kr[kDepth][NLD], vr[kDepth][NLD];
+      uint32_t sc[kDepth];
+      // row `r` (0 .. 31) of the wave's j-th tile
+      auto row_of = [&](int j, int r) {
+        return Lists ? my_rows[j * kTile + r] : min(c0 + (t0 + j) * kTile + r, c1 - 1);
+      };
+      auto fetch = [&](v4u (&kx)[NLD], v4u (&vx)[NLD], uint32_t& sx, int j) {
+        const uint32_t lane_o = opaque(lane);
+        sx = sbase[uint32_t(row_of(j, lane_o & 31)) >> c.shift];
 #pragma unroll
-      for (int n = 0; n < NQ4; ++n) {
-        float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = 0; i < NLD; ++i) {
+          const uint32_t off = __umul24(uint32_t(row_of(j, (i * 64 + lane_o) / CC)), pitch) + coff;
+          kx[i] = load_once(kbase + off);
+          vx[i] = load_once(vbase + off);
+        }
+      };
+#pragma unroll
+      for (int d = 0; d < kDepth; ++d)
+        if (d < mine) fetch(kr[d], vr[d], sc[d], d);
+      for (int j0 = 0; j0 < mine; j0 += kDepth) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+          const int j = j0 + d, tile = t0 + j;
+          if (j < mine) {
+            VtAddr<D> vtr;
+            vtr.base[0] = opaque(vt.base[0]);
+            vtr.base[1] = opaque(vt.base[1]);
+            const uint32_t lane_o = opaque(lane);
+            const u32x2 both = __builtin_amdgcn_permlane32_swap(sc[d], sc[d], false, false);
+            const float ku = scale_of(both[0]);   // of K row col, in both halves
+#pragma unroll
+            for (int i = 0; i < NLD; ++i) {
+              const uint32_t f = i * 64 + lane_o, r = f / CC, cc = f % CC;
+              const float vu = scale_of(uint32_t(__builtin_amdgcn_ds_bpermute(int(r * 4 + 128), int(sc[d]))));
+              *reinterpret_cast<v4u*>(ktile + codes_off<D>(r, cc)) = kr[d][i];
+              v4u lo, hi;
+              widen_codes(vr[d][i], vu, lo, hi);
+              *reinterpret_cast<v4u*>(vtile + tile_off<D>(r, cc)) = lo;
+              *reinterpret_cast<v4u*>(vtile + tile_off<D>(r, cc + CC)) = hi;
+            }
+            if (j + kDepth < mine) fetch(kr[d], vr[d], sc[d], j + kDepth);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            // every operand is asked for at once, V's before the softmax that stands between
+            v4u kx[NT / 2], vx[2][NDB];
+            const int ko = opaque(koff);
+#pragma unroll
+            for (int u = 0; u < NT / 2; ++u) kx[u] = *reinterpret_cast<const v4u*>(ktile + (ko ^ (u << 5)));
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int db = 0; db < NDB; ++db) {
+                const v2u lo = lds_read_tr16(vtile + vtr.off(0, db) + 16 * u * 2 * D);
+                const v2u hi = lds_read_tr16(vtile + vtr.off(1, db) + 16 * u * 2 * D);
+                vx[u][db] = v4u{lo.x, lo.y, hi.x, hi.y};
+              }
+            f32x16 st;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st[i] = 0.0f;
+#pragma unroll
+            for (int u = 0; u < NT / 2; ++u) {
+              v4u lo, hi;
+              widen_codes(kx[u], ku, lo, hi);
+              st = mfma_bf16(lo, qx[2 * u], st);
+              st = mfma_bf16(hi, qx[2 * u + 1], st);
+            }
+            v4u pb[2];
+            softmax_step(st, hf, c1 - (c0 + tile * kTile), zscale, m_used, lsum, acc, pb);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int db = 0; db < NDB; ++db) acc[db] = mfma_bf16(vx[u][db], pb[u], acc[db]);
+            __builtin_amdgcn_wave_barrier();
+          }
+        }
+      }
+
+      // ---- merge the waves' (m, l, O^T) through LDS that only they have used (as in attend_sparse_bf16_kernel)
+      const float l = sum_across_halves(lsum);
+      float* sm_ml = reinterpret_cast<float*>(&sm_rows[0][0]);   // [wave][m: 32 | l: 32], row stride kMl
+      if (hf == 0) {
+        sm_ml[wave * kMl + col] = m_used;
+        sm_ml[wave * kMl + 32 + col] = l;
+      }
+      float4* mrg = reinterpret_cast<float4*>(&lds[0][0]);
+      constexpr int kMrgWave = WAVEB / 16;
+      static_assert(NDB * 4 * 64 <= kMrgWave, "a wave's accumulators fit its tile buffers");
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4)
+          mrg[wave * kMrgWave + (db * 4 + i4) * 64 + lane] =
+              make_float4(acc[db][4 * i4 + 0], acc[db][4 * i4 + 1], acc[db][4 * i4 + 2], acc[db][4 * i4 + 3]);
+      __syncthreads();
+      {
+        constexpr int PARTS = W / NDB, NQ4 = 4 / PARTS;
+        static_assert(W % NDB == 0 && 4 % PARTS == 0, "the waves split the output evenly");
+        const int db = wave % NDB, i4_0 = (wave / NDB) * NQ4;
+        float m_all = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) m_all = fmaxf(m_all, sm_ml[w * kMl + col]);
+        float f[W];
+        float l_all = 0.0f;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-          const float4 y = mrg[w * kMrgWave + (db * 4 + i4_0 + n) * 64 + lane];
-          a.x += y.x * f[w]; a.y += y.y * f[w]; a.z += y.z * f[w]; a.w += y.w * f[w];
+          f[w] = __builtin_amdgcn_exp2f(sm_ml[w * kMl + col] - m_all);   // 0 for a wave that saw no tile
+          l_all += sm_ml[w * kMl + 32 + col] * f[w];
         }
-        const int at = db * 32 + 8 * (i4_0 + n) + 4 * hf;
-        if (x < ncols) {
-          if (cg.n == 1) {
-            *reinterpret_cast<v2u*>(o + row * D + at) = v2u{cvt_pk_bf16(a.x * inv, a.y * inv), cvt_pk_bf16(a.z * inv, a.w * inv)};
-          } else {
-            const int64_t part = int64_t(chunk) * s.total_q * s.hq + row;
-            *reinterpret_cast<float4*>(po + part * D + at) = a;
-            if (n == 0 && wave == 0 && hf == 0) { pm[part] = m_all; pl[part] = l_all; }
+        const int x = qt * 32 + col;
+        const int qi = query_of(x);
+        const int64_t row = int64_t(sg.q0 + qi) * s.hq + h0 + (x - qi * heads);
+        const float inv = 1.0f / l_all;
+#pragma unroll
+        for (int n = 0; n < NQ4; ++n) {
+          float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int w = 0; w < W; ++w) {
+            const float4 y = mrg[w * kMrgWave + (db * 4 + i4_0 + n) * 64 + lane];
+            a.x += y.x * f[w]; a.y += y.y * f[w]; a.z += y.z * f[w]; a.w += y.w * f[w];
+          }
+          const int at = placed<D>(db * 4 + i4_0 + n) * 8 + 4 * hf;
+          if (x < ncols) {
+            if (!Pieces || sg.parts == 1) {
+              *reinterpret_cast<v2u*>(o + row * D + at) =
+                  v2u{cvt_pk_bf16(a.x * inv, a.y * inv), cvt_pk_bf16(a.z * inv, a.w * inv)};
+            } else {
+              // (pieces and sequences only ever go up along a head's lists, so px + b numbers the segments)
+              const int64_t slot = (int64_t(px + sg.b) * s.max_q + qi) * s.hq + h0 + (x - qi * heads);
+              *reinterpret_cast<float4*>(po + slot * D + at) = a;
+              if (n == 0 && wave == 0 && hf == 0) pml[slot] = make_float2(m_all, l_all);
+            }
           }
         }
       }
+      __syncthreads();   // merge space becomes tile space again
     }
-    if ((qt + qstep) * 32 < ncols) __syncthreads();   // merge space becomes tile space again
+    if constexpr (!Pieces) break;
+    else {
+      if (sg.k0 + sg.c1 >= end) break;
+      enter(sg.b + 1);   // (there is one: the piece goes on)
+    }
   }
 }
 
-// How a call's rows are shared out over the compute units (see plan_attend, whose sums these are with this kernel's rates).
-static AttendPlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k) {
-  AttendPlan p{};
-  p.chunk_rows = max_k > 0 ? max_k : 1;
-  p.n_chunks = 1;
-  p.max_k = max_k;
-  p.v_split = 1;
-  if (max_k > 0) {
-    const int64_t heads = lists ? s.hq : s.hkv, cols = lists ? s.max_q : int64_t(s.max_q) * s.group;
-    const int64_t units = int64_t(s.batch) * heads * std::max<int64_t>(1, (cols + 31) / 32);
-    int64_t n = std::max<int64_t>(1, 512 / std::max<int64_t>(1, units));
-    n = std::max<int64_t>(1, std::min<int64_t>(n, max_k / 256));
-    p.chunk_rows = int32_t(((max_k + n - 1) / n + 127) / 128 * 128);
-    if (lists) p.chunk_rows = std::min(p.chunk_rows, kMaxChunkRows);
-    p.n_chunks = int32_t((int64_t(max_k) + p.chunk_rows - 1) / p.chunk_rows);
+// Merges the parts of every list that a cut went through: one thread per four output elements, the parts of four pieces asked
+// for at once, and PG groups of threads that share out the parts of a row where there are many (few rows, then).
+template <int D, int PG>
+__global__ __launch_bounds__(256) void merge_pieces_kernel(const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
+                                                           const float* __restrict__ po, const float2* __restrict__ pml,
+                                                           uint16_t* __restrict__ o, int32_t piece, Shape s DLLM_CHECK_PARAM) {
+  DLLM_CHECK_EXIT();
+  constexpr int TPR = D / 4, ROWS = 256 / TPR / PG;   // threads per output row and group, rows per workgroup and turn
+  __shared__ float4 sm_a[PG > 1 ? 256 : 1];
+  __shared__ float2 sm_ml[PG > 1 ? 256 : 1];
+  const int b = blockIdx.y;
+  const int k0 = cu_k[b], k1 = cu_k[b + 1], q0 = cu_q[b], n = (cu_q[b + 1] - q0) * s.hq;
+  const int fp = int(uint32_t(k0) / uint32_t(piece)), parts = k1 > k0 ? int(uint32_t(k1 - 1) / uint32_t(piece)) - fp + 1 : 0;
+  if (parts <= 1) return;
+  const int sub = threadIdx.x % TPR, pg = threadIdx.x / TPR % PG;
+  const int64_t pitch = int64_t(s.max_q) * s.hq;   // slot of part p: base + row + p * pitch
+  const int64_t base = (int64_t(fp) + b) * pitch;
+  for (int i0 = blockIdx.x * ROWS; i0 < n; i0 += gridDim.x * ROWS) {
+    const int i = i0 + int(threadIdx.x) / (TPR * PG);
+    const int64_t row = min(i, n - 1);
+    float m_all = -INFINITY, l_all = 0.0f;
+    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int p0 = 4 * pg; p0 < parts; p0 += 4 * PG) {
+      float2 ml[4];
+      float4 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {   // past the last part: that part again, with no weight
+        const int64_t slot = base + row + min(p0 + u, parts - 1) * pitch;
+        ml[u] = pml[slot];
+        x[u] = *reinterpret_cast<const float4*>(po + slot * D + sub * 4);
+      }
+      float m_new = m_all;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) m_new = fmaxf(m_new, ml[u].x);
+      const float old = __builtin_amdgcn_exp2f(m_all - m_new);   // first round: exp2(-inf) = 0
+      l_all *= old;
+      a.x *= old; a.y *= old; a.z *= old; a.w *= old;
+      m_all = m_new;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float w = p0 + u < parts ? __builtin_amdgcn_exp2f(ml[u].x - m_all) : 0.0f;
+        l_all += ml[u].y * w;
+        a.x += x[u].x * w; a.y += x[u].y * w; a.z += x[u].z * w; a.w += x[u].w * w;
+      }
+    }
+    if constexpr (PG > 1) {
+      sm_a[threadIdx.x] = a;
+      sm_ml[threadIdx.x] = make_float2(m_all, l_all);
+      __syncthreads();
+      const int first = threadIdx.x - pg * TPR;
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < PG; ++w) m = fmaxf(m, sm_ml[first + w * TPR].x);
+      a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      l_all = 0.0f;
+#pragma unroll
+      for (int w = 0; w < PG; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sm_ml[first + w * TPR].x - m);   // 0 for a group without parts
+        const float4 y = sm_a[first + w * TPR];
+        l_all += sm_ml[first + w * TPR].y * f;
+        a.x += y.x * f; a.y += y.y * f; a.z += y.z * f; a.w += y.w * f;
+      }
+      __syncthreads();
+    }
+    if (i < n && pg == 0) {
+      const float inv = 1.0f / l_all;
+      *reinterpret_cast<v2u*>(o + (int64_t(q0) * s.hq + row) * D + sub * 4) =
+          v2u{cvt_pk_bf16(a.x * inv, a.y * inv), cvt_pk_bf16(a.z * inv, a.w * inv)};
+    }
   }
-  if (p.n_chunks > 1) {
-    const size_t slots = size_t(p.n_chunks) * size_t(s.total_q) * size_t(s.hq);
-    p.off_po = 0;
-    p.off_pm = align256(slots * s.d * sizeof(float));
-    p.off_pl = p.off_pm + align256(slots * sizeof(float));
-    p.bytes = p.off_pl + align256(slots * sizeof(float));
+}
+
+// How a call's rows are shared out: in pieces of `piece` rows, or (0) a list per workgroup.
+struct CachePlan {
+  int32_t piece, n_pieces;   // per head
+  int64_t groups;            // workgroups that share the column tiles of a sequence
+  int order;
+};
+// Pieces are cut for one workgroup per compute unit at head_dim 128, two at 64.
+static int64_t pieces_per_head(const Shape& s, int64_t units) {
+  return std::max<int64_t>(1, (s.d == 128 ? kUnits : 2 * kUnits) / units);
+}
+// Lists whole or in pieces: the less of two sums, in us, from these measurements.
+//   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6), two on one unit 0.7 of their sum; the card reads gathered rows at
+//   4.9 TB/s, rows in order at 5.0, at 4.2 where every list is a workgroup's own (64-byte rows two thirds of that; all of it
+//   includes starting and draining).
+//   Pieces cost a second launch and its latencies (3.3), what is written and read again (2.75 TB/s), and 1.4 for each further sequence that
+//   a piece reaches into.
+// One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 20.8 / 9.5; 32 of 4000 to 8192 78.9 / 73.2;
+// 16 of 1000 13.5 / 16.1; 40 of 100 to 1000 19.8 / 23.3; lists of 32 heads x 128, one of 4096 rows 25.9 / 14.5, of 512 9.2 / 9.5, of 256 7.0 / 9.7; four
+// of 276 to 994 12.8 / 16.9; sixteen of 5 to 50 % of 512 to 4096 28.9 / 36.3.  Over 640 batches, 1 to 40 sequences of 128 to 8192, the
+// choice is 0.3 % above the better one in the mean, 37 % at most (one list of 1021 rows over 32 heads).
+static bool better_in_pieces(const Shape& s, bool lists, int64_t heads, int64_t cols, int64_t tiles, int64_t max_k, int64_t total_k,
+                             int64_t piece) {
+  const double row_us = s.d == 128 ? 7.0e-3 : 4.6e-3, units = double(heads * tiles), n = double((total_k + piece - 1) / piece);
+  const double read = double(total_k) * heads * 2 * s.d / (lists ? 4.9e6 : 5.0e6) * (s.d == 128 ? 1.0 : 1.5);
+  double whole = max_k * row_us;
+  if (units * s.batch > kUnits) whole = std::max(whole, total_k * units / kUnits * row_us * 0.7);
+  whole = std::max(whole, lists ? read : read * 1.2);
+  double cut = piece * row_us;
+  if (units * n > kUnits) cut *= s.d == 128 ? 1.4 : 1.3;
+  cut = std::max(cut, read) + 3.3 + 1.4 * (s.batch - 1) / n;
+  cut += (n + s.batch) * units * std::min<int64_t>(32, cols) * s.d * 8 / 2.75e6;
+  return cut < whole;
+}
+static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, int64_t total_k) {
+  CachePlan p{};
+  total_k = std::min<int64_t>(total_k, int64_t(s.batch) * max_k);
+  const int64_t heads = lists ? s.hq : s.hkv, cols = lists ? s.max_q : int64_t(s.max_q) * s.group;
+  const int64_t tiles = std::max<int64_t>(1, (cols + 31) / 32), units = heads * tiles, resident = 2 * kUnits;
+  if (max_k > 0) {
+    const int64_t share = (total_k + pieces_per_head(s, units) - 1) / pieces_per_head(s, units);
+    int64_t piece = std::max<int64_t>(128, (share + 31) / 32 * 32);
+    // (the ids of a list's rows lie in LDS: no workgroup takes more than kMaxListRows of them, whole or in pieces)
+    bool cut = lists && max_k > kMaxListRows;
+    if (!cut && !(lists && piece > kMaxListRows)) cut = better_in_pieces(s, lists, heads, cols, tiles, max_k, total_k, piece);
+    if (lists) piece = std::min<int64_t>(piece, kMaxListRows);
+    if (cut) {
+      p.piece = int32_t(std::min<int64_t>(piece, INT32_MAX));
+      p.n_pieces = int32_t((total_k + p.piece - 1) / p.piece);
+    }
+  }
+  const int64_t wgs = heads * (p.piece ? p.n_pieces : s.batch);
+  p.groups = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles, 65535), resident / std::max<int64_t>(1, wgs)));
+  if (!p.piece && s.batch <= kRankBatch && p.groups == 1) {
+    if (wgs > resident) p.order = kLongestFirst;
+    else if (wgs > kUnits) p.order = kFolded;
   }
   return p;
 }
+int32_t attend_cached_piece(const Shape& s, bool lists, int32_t max_k, int32_t total_k) {
+  return plan_attend_cached(s, lists, max_k, total_k).piece;
+}
+static size_t partial_slots(const Shape& s, int64_t n_pieces) {
+  return size_t(n_pieces + s.batch) * size_t(s.max_q) * size_t(s.hq);
+}
 
 size_t attend_cached_workspace(const Shape& s, int32_t max_k) {
-  return std::max(plan_attend_cached(s, true, max_k).bytes, plan_attend_cached(s, false, max_k).bytes);
+  if (max_k == 0 || s.max_q == 0) return 0;
+  const int64_t tiles = (int64_t(s.max_q) + 31) / 32, group_tiles = (int64_t(s.max_q) * s.group + 31) / 32;
+  int64_t n = std::max(pieces_per_head(s, s.hq * tiles), pieces_per_head(s, s.hkv * group_tiles));
+  if (max_k > kMaxListRows) n = std::max<int64_t>(n, (int64_t(s.batch) * max_k + kMaxListRows - 1) / kMaxListRows);
+  const size_t slots = partial_slots(s, n);
+  return align256(slots * s.d * sizeof(float)) + align256(slots * sizeof(float2));
 }
 
 hipError_t launch_attend_cached(const Shape& s, const CacheView& c, int32_t max_k, const void* q, const int32_t* cu_q,
                                 const int32_t* cu_kv, const int32_t* idx, const int32_t* cu_k, int32_t total_k, void* o, void* ws,
                                 hipStream_t st) {
   if (s.max_q == 0) return hipSuccess;   // no sequence has a query: nothing to write
-  const AttendPlan p = plan_attend_cached(s, idx != nullptr, max_k);
-  char* w = static_cast<char*>(ws);
-  float* po = p.n_chunks > 1 ? reinterpret_cast<float*>(w + p.off_po) : nullptr;
-  float* pm = p.n_chunks > 1 ? reinterpret_cast<float*>(w + p.off_pm) : nullptr;
-  float* pl = p.n_chunks > 1 ? reinterpret_cast<float*>(w + p.off_pl) : nullptr;
+  const bool lists = idx != nullptr;
+  const CachePlan p = plan_attend_cached(s, lists, max_k, total_k);
+  float* po = static_cast<float*>(ws);
+  float2* pml = reinterpret_cast<float2*>(static_cast<char*>(ws) + align256(partial_slots(s, p.n_pieces) * s.d * sizeof(float)));
   const uint16_t* qh = static_cast<const uint16_t*>(q);
   uint16_t* oh = static_cast<uint16_t*>(o);
-  const bool lists = idx != nullptr;
-  const int64_t heads = lists ? s.hq : s.hkv, cols = lists ? s.max_q : int64_t(s.max_q) * s.group;
-  const int64_t units = int64_t(p.n_chunks) * heads * s.batch, tiles = (cols + 31) / 32;
-  const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles, 65535 / s.batch), 512 / units));
-  const dim3 grid(p.n_chunks, unsigned(heads), unsigned(s.batch * groups));
-  const int ranked = units * groups > 512 ? 1 : 0;
-  auto launch = [&](auto kernel) {
-    kernel<<<grid, kWaves * 64, 0, st>>>(qh, c, cu_q, cu_kv, idx, cu_k, total_k, oh, po, pm, pl, p.chunk_rows, ranked,
-                                         s DLLM_CHECK_PASS);
+  // Without lists the heads of one piece run on one XCD if the number of pieces is a multiple of eight: their rows lie side by side.
+  const unsigned heads = lists ? s.hq : s.hkv;
+  const unsigned parts = !p.piece ? s.batch : lists || p.n_pieces < 8 ? p.n_pieces : (p.n_pieces + 7) / 8 * 8;
+  auto launch = [&](auto kernel, bool heads_first) {
+    const dim3 grid(heads_first ? heads : parts, heads_first ? parts : heads, unsigned(p.groups));
+    kernel<<<grid, kWaves * 64, 0, st>>>(qh, c, cu_q, cu_kv, idx, cu_k, total_k, oh, po, pml, p.piece, p.order, s DLLM_CHECK_PASS);
   };
   auto with_d = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (lists) {
-      if (groups > 1) launch(attend_cache_kernel<D, true, true>);
-      else launch(attend_cache_kernel<D, true, false>);
+    if (p.piece) {
+      if (lists) launch(attend_cache_kernel<D, true, true>, true);
+      else launch(attend_cache_kernel<D, false, true>, false);
     } else {
-      if (groups > 1) launch(attend_cache_kernel<D, false, true>);
-      else launch(attend_cache_kernel<D, false, false>);
+      if (lists) launch(attend_cache_kernel<D, true, false>, true);
+      else launch(attend_cache_kernel<D, false, false>, true);
     }
   };
   if (s.d == 128) with_d(std::integral_constant<int, 128>{});
   else with_d(std::integral_constant<int, 64>{});
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_chunks <= 1) return e;
-  return launch_merge_chunks(s, p, cu_q, cu_k, nullptr, po, pm, pl, oh, st);
+  if (e != hipSuccess || !p.piece) return e;
+  auto merge = [&](auto kernel, int rows_per_wg) {
+    const int64_t wgs = (int64_t(s.max_q) * s.hq + rows_per_wg - 1) / rows_per_wg;
+    const dim3 grid(unsigned(std::min<int64_t>(wgs, std::max<int64_t>(4, 4096 / s.batch))), s.batch);
+    kernel<<<grid, 256, 0, st>>>(cu_q, cu_k, po, pml, oh, p.piece, s DLLM_CHECK_PASS);
+  };
+  const bool many = (int64_t(max_k) + p.piece - 1) / p.piece + 1 > 8;   // parts of the longest list
+  if (s.d == 128) {
+    if (many) merge(merge_pieces_kernel<128, 8>, 1);
+    else merge(merge_pieces_kernel<128, 1>, 8);
+  } else {
+    if (many) merge(merge_pieces_kernel<64, 8>, 2);
+    else merge(merge_pieces_kernel<64, 1>, 16);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace dllm

@@ -1,6 +1,5 @@
 // What the attention kernels over kept rows share (bf16 rows: attend_sparse_bf16.hip; rows of an 8-bit cache:
-// attend_cache.hip): how a list is cut into chunks, the batch's offsets in one workgroup, and the arithmetic on one
-// 32-row tile that lies in LDS as bf16.
+// attend_cache.hip): the batch's offsets in one workgroup, and the online softmax of one 32-row tile.
 #pragma once
 #include "attn_tile.h"
 
@@ -8,22 +7,6 @@ namespace dllm {
 
 constexpr int kTile = 32;             // kept rows per wave tile
 constexpr int kRankBatch = 64;        // batches up to this size are walked longest kept list first
-
-// A (sequence, head) with kb kept rows is cut into n = ceil(kb / chunk_rows) chunks of equal size
-// (rounded up to the 128 rows four waves take per step), so no chunk is a short leftover.
-struct ChunkGeom {
-  int n, rows;
-};
-__device__ __forceinline__ ChunkGeom chunk_geom(int kb, int chunk_rows) {
-  ChunkGeom g;
-  g.n = 1;
-  g.rows = chunk_rows;
-  if (kb > chunk_rows) {
-    g.n = int(uint32_t(kb + chunk_rows - 1) / uint32_t(chunk_rows));
-    g.rows = int((uint32_t(kb + g.n - 1) / uint32_t(g.n) + 127u) / 128u * 128u);
-  }
-  return g;
-}
 
 // Per-sequence offsets a workgroup needs, fetched for the whole (small) batch in one round of
 // loads: lane i holds sequence i's entries, and the chosen sequence's are read back by lane index.
@@ -89,31 +72,12 @@ __device__ __forceinline__ SeqInfo sequence_of_slot(const int32_t* __restrict__ 
                           ranked);
 }
 
-// One 32-key tile that lies in LDS (K rows in ktile, V rows in vtile, the 32 queries in qtile, all in the
-// swizzled tile layout): S^T = K Q^T, online softmax over the first nvalid keys, O^T += V^T P^T for the NDB blocks
-// of 32 head_dim elements that `vt` starts at.
-template <int D, int NDB = D / 32>
-__device__ __forceinline__ void sparse_tile_math(const char* ktile, const char* vtile, const char* qtile,
-                                                 const KAddr<D>& ka, const VtAddr<D>& vt, int hf, int nvalid,
-                                                 float zscale, float& m_used, float& lsum, f32x16 (&acc)[NDB]) {
-  constexpr int ROWB = 2 * D;
-  constexpr int NT = D / 16;    // MFMA steps along head_dim
-  // S^T tile: rows = keys, columns = queries
-  f32x16 st;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) st[i] = 0.0f;
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-    st = mfma_bf16(*reinterpret_cast<const v4u*>(ktile + ka.off(t)),
-                   *reinterpret_cast<const v4u*>(qtile + ka.off(t)), st);
-  // issue order: operand fetches just ahead of their MFMA, so few operand registers are live
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-  }
-  __builtin_amdgcn_sched_barrier(0);
-
+// Online softmax of one 32-key tile: S^T (rows: keys, columns: queries) becomes the bf16 operand P^T of the product with V^T; the
+// running maximum and sum of this lane's column, and the accumulators where the maximum is raised, follow.  Keys from
+// nvalid on count nothing.
+template <int NDB>
+__device__ __forceinline__ void softmax_step(f32x16 st, int hf, int nvalid, float zscale, float& m_used, float& lsum,
+                                             f32x16 (&acc)[NDB], v4u (&pb)[2]) {
   if (nvalid < kTile) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -136,7 +100,6 @@ __device__ __forceinline__ void sparse_tile_math(const char* ktile, const char* 
       for (int i = 0; i < 16; ++i) acc[db][i] *= alpha;
   }
   const float neg_m = -m_used;
-  v4u pb[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     uint32_t w[4];
@@ -148,21 +111,6 @@ __device__ __forceinline__ void sparse_tile_math(const char* ktile, const char* 
       lsum = add_pair_bf16(w[jj], lsum);
     }
     pb[u] = v4u{w[0], w[1], w[2], w[3]};
-  }
-  // O^T += V^T P^T, 16 keys per step
-  __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      const v2u lo = lds_read_tr16(vtile + vt.off(0, db) + 16 * u * ROWB);
-      const v2u hi = lds_read_tr16(vtile + vt.off(1, db) + 16 * u * ROWB);
-      acc[db] = mfma_bf16(v4u{lo.x, lo.y, hi.x, hi.y}, pb[u], acc[db]);
-    }
-#pragma unroll
-  for (int i = 0; i < 2 * NDB; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
   }
 }
 

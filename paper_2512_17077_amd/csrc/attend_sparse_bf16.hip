@@ -48,6 +48,67 @@ __device__ __forceinline__ int later_tile(int wave, int k) {
   const int p = k / S, r = k % S;
   return kWavesMulti + P * p + 8 * r + wave;
 }
+
+// A (sequence, head) with kb kept rows is cut into n = ceil(kb / chunk_rows) chunks of equal size
+// (rounded up to the 128 rows four waves take per step), so no chunk is a short leftover.
+struct ChunkGeom {
+  int n, rows;
+};
+__device__ __forceinline__ ChunkGeom chunk_geom(int kb, int chunk_rows) {
+  ChunkGeom g;
+  g.n = 1;
+  g.rows = chunk_rows;
+  if (kb > chunk_rows) {
+    g.n = int(uint32_t(kb + chunk_rows - 1) / uint32_t(chunk_rows));
+    g.rows = int((uint32_t(kb + g.n - 1) / uint32_t(g.n) + 127u) / 128u * 128u);
+  }
+  return g;
+}
+
+// One 32-key tile that lies in LDS (K rows in ktile, V rows in vtile, the 32 queries in qtile, all in the
+// swizzled tile layout): S^T = K Q^T, online softmax over the first nvalid keys, O^T += V^T P^T for the NDB blocks
+// of 32 head_dim elements that `vt` starts at.
+template <int D, int NDB = D / 32>
+__device__ __forceinline__ void sparse_tile_math(const char* ktile, const char* vtile, const char* qtile,
+                                                 const KAddr<D>& ka, const VtAddr<D>& vt, int hf, int nvalid,
+                                                 float zscale, float& m_used, float& lsum, f32x16 (&acc)[NDB]) {
+  constexpr int ROWB = 2 * D;
+  constexpr int NT = D / 16;    // MFMA steps along head_dim
+  // S^T tile: rows = keys, columns = queries
+  f32x16 st;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) st[i] = 0.0f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    st = mfma_bf16(*reinterpret_cast<const v4u*>(ktile + ka.off(t)),
+                   *reinterpret_cast<const v4u*>(qtile + ka.off(t)), st);
+  // issue order: operand fetches just ahead of their MFMA, so few operand registers are live
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+
+  v4u pb[2];
+  softmax_step(st, hf, nvalid, zscale, m_used, lsum, acc, pb);
+  // O^T += V^T P^T, 16 keys per step
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      const v2u lo = lds_read_tr16(vtile + vt.off(0, db) + 16 * u * ROWB);
+      const v2u hi = lds_read_tr16(vtile + vt.off(1, db) + 16 * u * ROWB);
+      acc[db] = mfma_bf16(v4u{lo.x, lo.y, hi.x, hi.y}, pb[u], acc[db]);
+    }
+#pragma unroll
+  for (int i = 0; i < 2 * NDB; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+  }
+}
+
 // Once: K and V rows are read with the non-temporal hint (gathers_once)
 // VS: workgroups per list, each of which takes all of the K rows and 1 / VS of head_dim of the V rows and of the
 // output (see plan_attend); they are VS consecutive values of blockIdx.z, so with a multiple of eight heads
@@ -645,30 +706,6 @@ __global__ __launch_bounds__(256) void attend_sparse_combine_kernel(
   } while (Turns && i < nq);
 }
 
-hipError_t launch_merge_chunks(const Shape& s, const AttendPlan& p, const int32_t* cu_q, const int32_t* cu_k,
-                               const uint8_t* seq_mode, const float* po, const float* pm, const float* pl, void* o,
-                               hipStream_t st) {
-  uint16_t* oh = static_cast<uint16_t*>(o);
-  // The longest sequence may be one that is attended densely, with thousands of queries and nothing to merge: no more
-  // than about 2048 workgroups are started beyond the four per list that a block of 32 queries takes, and they loop
-  // (8 x 32 lists of 3200 kept rows, two sequences dense with 2048 queries: 25 us with a workgroup per eight rows of
-  // max_q, 5 us like this).
-  const int rows = 256 / (s.d / 4);
-  const int64_t lists = int64_t(s.hq) * s.batch, most = std::max<int64_t>(4, 2048 / lists), all = (s.max_q + rows - 1) / rows;
-  auto combine = [&](auto kernel) {
-    kernel<<<dim3(unsigned(std::min(all, most)), s.hq, s.batch), 256, 0, st>>>(cu_q, cu_k, seq_mode, po, pm, pl, oh,
-                                                                               p.chunk_rows, s DLLM_CHECK_PASS);
-  };
-  if (s.d == 128) {
-    if (all <= most) combine(attend_sparse_combine_kernel<128, false>);
-    else combine(attend_sparse_combine_kernel<128, true>);
-  } else {
-    if (all <= most) combine(attend_sparse_combine_kernel<64, false>);
-    else combine(attend_sparse_combine_kernel<64, true>);
-  }
-  return hipGetLastError();
-}
-
 hipError_t launch_attend_sparse_bf16(const Shape& s, const AttendPlan& p, const void* q, const void* k,
                                      const void* v, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* idx,
                                      const int32_t* cu_k, int32_t total_k, const uint8_t* seq_mode, void* o,
@@ -739,7 +776,24 @@ hipError_t launch_attend_sparse_bf16(const Shape& s, const AttendPlan& p, const 
   }
   e = hipGetLastError();
   if (e != hipSuccess || p.n_chunks <= 1) return e;
-  return launch_merge_chunks(s, p, cu_q, cu_k, seq_mode, po, pm, pl, oh, st);
+  // The longest sequence may be one that is attended densely, with thousands of queries and nothing to merge: no more
+  // than about 2048 workgroups are started beyond the four per list that a block of 32 queries takes, and they loop
+  // (8 x 32 lists of 3200 kept rows, two sequences dense with 2048 queries: 25 us with a workgroup per eight rows of
+  // max_q, 5 us like this).
+  const int rows = 256 / (s.d / 4);
+  const int64_t lists = int64_t(s.hq) * s.batch, most = std::max<int64_t>(4, 2048 / lists), all = (s.max_q + rows - 1) / rows;
+  auto combine = [&](auto kernel) {
+    kernel<<<dim3(unsigned(std::min(all, most)), s.hq, s.batch), 256, 0, st>>>(cu_q, cu_k, seq_mode, po, pm, pl, oh,
+                                                                               p.chunk_rows, s DLLM_CHECK_PASS);
+  };
+  if (s.d == 128) {
+    if (all <= most) combine(attend_sparse_combine_kernel<128, false>);
+    else combine(attend_sparse_combine_kernel<128, true>);
+  } else {
+    if (all <= most) combine(attend_sparse_combine_kernel<64, false>);
+    else combine(attend_sparse_combine_kernel<64, true>);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace dllm

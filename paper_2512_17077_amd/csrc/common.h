@@ -106,14 +106,11 @@ hipError_t launch_attend_sparse_bf16(const Shape& s, const AttendPlan& p, const 
                                      const int32_t* cu_k, int32_t total_k, const uint8_t* seq_mode, void* o,
                                      void* ws, hipStream_t st);
 // The same over an 8-bit cache; without lists (idx NULL) all heads attend over the first rows of their sequence.
+int32_t attend_cached_piece(const Shape& s, bool lists, int32_t max_k, int32_t total_k);   // rows per piece; 0: every list whole
 size_t attend_cached_workspace(const Shape& s, int32_t max_k);   // enough for a call with lists and for one without
 hipError_t launch_attend_cached(const Shape& s, const CacheView& c, int32_t max_k, const void* q, const int32_t* cu_q,
                                 const int32_t* cu_kv, const int32_t* idx, const int32_t* cu_k, int32_t total_k, void* o, void* ws,
                                 hipStream_t st);
-// merges the partial results of lists that were cut into chunks
-hipError_t launch_merge_chunks(const Shape& s, const AttendPlan& p, const int32_t* cu_q, const int32_t* cu_k,
-                               const uint8_t* seq_mode, const float* po, const float* pm, const float* pl, void* o,
-                               hipStream_t st);
 hipError_t launch_attend_dense_bf16(const Shape& s, const void* q, const void* k, const void* v,
                                     const int32_t* cu_q, const int32_t* cu_kv, const uint8_t* seq_mode, int which,
                                     void* o, hipStream_t st);

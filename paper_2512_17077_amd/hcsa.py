@@ -34,7 +34,7 @@ EXPORTS = [
     "dllm_hcsa_pack", "dllm_hcsa_precondition_errors",
     "dllm_hcsa_cache_scale_slots", "dllm_hcsa_cache_write", "dllm_hcsa_cache_read",
     "dllm_hcsa_select_cached_workspace", "dllm_hcsa_select_cached",
-    "dllm_hcsa_attend_cached_workspace", "dllm_hcsa_attend_cached",
+    "dllm_hcsa_attend_cached_workspace", "dllm_hcsa_attend_cached", "dllm_hcsa_attend_cached_form_of",
     "dllm_last_error", "dllm_hcsa_version",
 ]
 DLLM_CHECK_CU_Q, DLLM_CHECK_CU_KV, DLLM_CHECK_CU_K, DLLM_CHECK_K_OVER_L, DLLM_CHECK_FORCED, DLLM_CHECK_IDX = 1, 2, 4, 8, 16, 32
@@ -137,6 +137,8 @@ def lib() -> ctypes.CDLL:
         L.dllm_hcsa_select_cached.argtypes = [P, C, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp]
         L.dllm_hcsa_attend_cached_workspace.restype = sz
         L.dllm_hcsa_attend_cached_workspace.argtypes = [P, C, i32]
+        L.dllm_hcsa_attend_cached_form_of.restype = i32
+        L.dllm_hcsa_attend_cached_form_of.argtypes = [P, C, i32, i32, i32]
         L.dllm_hcsa_attend_cached.restype = ctypes.c_int
         L.dllm_hcsa_attend_cached.argtypes = [P, C, vp, vp, i32, i32, vp, vp, sz, vp]
         L.dllm_last_error.restype = ctypes.c_char_p
@@ -444,6 +446,15 @@ def dllm_hcsa_select_cached(batch: DllmBatch, cache: DllmCache, cu_k: torch.Tens
 
 def dllm_hcsa_attend_cached_workspace(batch: DllmBatch, cache: DllmCache, max_k: int) -> int:
     return int(lib().dllm_hcsa_attend_cached_workspace(ctypes.byref(batch), ctypes.byref(cache), int(max_k)))
+
+
+def dllm_hcsa_attend_cached_form_of(batch: DllmBatch, cache: DllmCache, lists: bool, max_k: int, total_k: int) -> int:
+    """Rows per piece in which a call cuts its lists, 0 if every list goes to a workgroup of its own."""
+    piece = int(lib().dllm_hcsa_attend_cached_form_of(ctypes.byref(batch), ctypes.byref(cache), int(bool(lists)), int(max_k),
+                                                      int(total_k)))
+    if piece < 0:
+        raise ValueError(last_error())
+    return piece
 
 
 def dllm_hcsa_attend_cached(batch: DllmBatch, cache: DllmCache, idx: Optional[torch.Tensor], cu_k: torch.Tensor, total_k: int,

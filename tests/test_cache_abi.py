@@ -170,9 +170,55 @@ def test_attend_cached_checks():
     b.max_kv = b.total_kv = 4000
     assert attend(b, c) == UNSUPPORTED
     c = good_cache()
+    b = good_batch()
+    assert attend(b, c, total=(1 << 27) + 1) == UNSUPPORTED and "2^27" in hcsa.last_error()
     b.max_kv = b.total_kv = (1 << 24) + 1
     c.scale_stride_head = 1 << 24
     assert attend(b, c) == UNSUPPORTED
+
+
+def shaped(rng):
+    b, c = good_batch(), good_cache()
+    d, group = rng.choice((64, 128)), rng.choice((1, 2, 4, 5, 8))
+    b.batch, b.n_kv_heads, b.head_dim = int(2 ** rng.uniform(0, 8)), rng.choice((1, 2, 4, 8, 16, 32)), d
+    b.n_q_heads = b.n_kv_heads * group
+    b.q_stride_tok, b.q_stride_head = b.n_q_heads * d, d
+    b.max_kv = int(2 ** rng.uniform(0, 14))
+    b.total_kv = b.max_kv + int((b.batch - 1) * b.max_kv * rng.random())
+    b.max_q = int(2 ** rng.uniform(0, 9))
+    b.total_q = b.max_q + int((b.batch - 1) * b.max_q * rng.random())
+    c.stride_tok, c.stride_head = b.n_kv_heads * d, d
+    c.scale_stride_head = b.total_kv // 32 + b.batch
+    return b, c, rng.randint(0, b.max_kv)
+
+
+def test_an_attend_call_never_takes_more_workspace_than_the_query_asks_for():
+    """The query does not know total_k nor whether there are lists: the segments that any call cuts have to fit what it said
+    (head_dim + 2 floats per segment, query and head; a head's lists have at most one segment per piece and one per sequence)."""
+    rng = random.Random(2)
+    whole = cut = 0
+    for _ in range(20000):
+        b, c, max_k = shaped(rng)
+        ws = hcsa.dllm_hcsa_attend_cached_workspace(b, c, max_k)
+        for total_k in {max_k, max_k + rng.randint(0, (b.batch - 1) * max_k), b.batch * max_k, b.batch * max_k + 70000}:
+            for lists in (False, True):
+                piece = hcsa.dllm_hcsa_attend_cached_form_of(b, c, lists, max_k, total_k)
+                whole, cut = whole + (piece == 0), cut + (piece > 0)
+                assert not (lists and max_k > 2048) or piece > 0   # (what one workgroup can take of a list)
+                assert not lists or piece <= 2048
+                if piece:
+                    pieces = -(-min(total_k, b.batch * max_k) // piece)
+                    assert ws >= (pieces + b.batch) * b.max_q * b.n_q_heads * (b.head_dim + 2) * 4, (b.batch, max_k, total_k, lists, piece)
+    assert whole > 10000 and cut > 10000
+
+
+def test_attend_form_of_checks_its_arguments():
+    b, c = good_batch(), good_cache()
+    for lists, max_k, total_k in ((2, 10, 10), (-1, 10, 10), (0, -1, 10), (0, 11, 10), (1, 4001, 5000), (0, 0, -1)):
+        assert hcsa.lib().dllm_hcsa_attend_cached_form_of(ctypes.byref(b), ctypes.byref(c), lists, max_k, total_k) == -1
+    b.head_dim = 96
+    with pytest.raises(ValueError):
+        hcsa.dllm_hcsa_attend_cached_form_of(b, c, True, 10, 10)
 
 
 def test_the_binding_refuses_tensors_that_do_not_fit():

@@ -460,6 +460,31 @@ def test_attention_of_more_lists_than_fit_at_once(lists):
     check_attend(filled(lens, 16, 64, 32, 83), 16, [16] * 40, [n // 2 for n in lens], 84, lists)
 
 
+def ragged(rng, n, lo, hi, empty=()):
+    return [0 if b in empty else int(x) for b, x in enumerate(rng.integers(lo, hi, n))]
+
+
+@pytest.mark.parametrize("lists", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,batch,lo,hi,nq,pieces", [
+    (16, 16, 64, 19, 50, 400, 2, False),     # all resident, more than one per compute unit: folded order
+    (12, 12, 128, 23, 50, 300, 1, False),    # ... with heads that do not divide the compute units
+    (6, 3, 64, 64, 5, 120, 3, False),        # as many sequences as are ranked
+    (9, 3, 64, 90, 5, 120, 3, False),        # more than are ranked
+    (1, 1, 64, 70, 300, 2500, 1, True),      # pieces over more sequences than a wave holds
+    (4, 2, 128, 33, 1, 3000, 2, True),       # pieces over many short and some long sequences
+    (2, 1, 128, 3, 2000, 9000, 17, True)])   # few lists: more than eight parts each
+def test_attention_in_every_form(hq, hkv, d, batch, lo, hi, nq, pieces, lists):
+    """Lists whole, in each of the orders they are started in, and in pieces; some sequences keep nothing, the first and last among
+    them."""
+    rng = np.random.default_rng(batch)
+    lens = ragged(rng, batch, lo, hi)
+    keep = [0 if b in (0, 3, batch - 1) else n for b, n in enumerate(lens)]
+    c = filled(lens, hkv, d, 32, 85)
+    b = hcsa.make_cached_batch(torch.zeros((nq * batch, hq, d), dtype=torch.bfloat16, device=DEV), c.cu_t, c.cu_t, c.total, hkv, nq, max(lens), 1)
+    assert (hcsa.dllm_hcsa_attend_cached_form_of(b, c.desc, lists, max(keep), sum(keep)) > 0) == pieces
+    check_attend(c, hq, [nq] * batch, keep, 86, lists)
+
+
 @pytest.mark.parametrize("lists", [True, False])
 def test_large_scores_and_strided_queries(lists):
     c = filled([400, 333], 2, 128, 32, 91, layout="padded")
