@@ -105,6 +105,27 @@ __device__ __forceinline__ float fma_chunk(float acc, float vq, const float (&kv
   }
 }
 
+// Scores of four query heads at once on the matrix cores (codes only): with v_mfma_f32_4x4x1_16b_f32, sixteen blocks of four heads by
+// four keys and one element of head_dim, register t of lane l is head t's sum for key l.  An element of the result is one fused
+// multiply-add in fp32 (denormals included), so 128 of them in order are the canonical chain, bit for bit (compared on 2 million
+// chains of 128 elements of all exponents).  8.4 cycles for four multiply-adds per lane, which take 19 on the vector units:
+// selection over 24 sequences of 8192 positions, 32 heads over 8 x 128, 58.7 -> 52.9 us, over one of 1024 10.1 -> 9.4.
+// Lane l's operand q4 holds the sums of head l % 4.
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+template <int N>
+__device__ __forceinline__ f32x4 mfma_chunk(f32x4 acc, const float* q4, const float (&kv)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; e += 4) {
+    const f32x4 q = *reinterpret_cast<const f32x4*>(q4 + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_4x4x1f32(q[i], kv[e + i], acc, 0, 0, 0);
+  }
+  return acc;
+}
+// Floats between the sums of two heads in LDS: where four heads are read side by side, four more than head_dim (other banks).
+template <int ES, int D, int GT>
+constexpr int kSumPitch = ES == 1 && GT == 4 ? D + 4 : D;
+
 // Scales of a cached K (8-bit cache only): scale bytes per KV head and block of 2^shift tokens.
 struct KeyScales {
   const uint8_t* at;
@@ -131,6 +152,8 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   constexpr int ROWB = D * ES;
   constexpr int CH = ROWB / 16;   // 16-byte chunks per row
   constexpr int EPC = 16 / ES;    // elements per chunk
+  constexpr bool kMatrix = ES == 1 && GT == 4;
+  constexpr int SD = kSumPitch<ES, D, GT>;
   __shared__ v4u tile[kScoreWaves][64 * CH];
   extern __shared__ __attribute__((aligned(16))) float sums[];   // [group][D]: block sums of this KV head's query heads
 
@@ -206,7 +229,7 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
         for (int j = 0; j < 16; ++j) a = a + x[j];
       }
       for (; i < nq; ++i) a = a + widen(p + i * qpitch);
-      sums[e] = a;
+      sums[e / D * SD + e % D] = a;
     }
     __syncthreads();
   }
@@ -215,13 +238,15 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   // vq[t][i] (the same in all four rows of 16 lanes).  With one pass per tile (group == GT) they are
   // read once, here; with several, at the start of every pass.
   constexpr int NQ = D / 16;
-  float vq[GT][NQ];
+  float vq[kMatrix ? 1 : GT][NQ];
   auto load_sums = [&](int hh) {
     const float* qs = sums + hh * D + (lane & 15);
+    if constexpr (!kMatrix) {
 #pragma unroll
-    for (int t = 0; t < GT; ++t)
+      for (int t = 0; t < GT; ++t)
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) vq[t][i] = qs[t * D + 16 * i];
+        for (int i = 0; i < NQ; ++i) vq[t][i] = qs[t * D + 16 * i];
+    }
   };
   const bool one_pass = s.group == GT;
   if (one_pass) load_sums(0);
@@ -245,16 +270,27 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
       float acc[GT];
 #pragma unroll
       for (int t = 0; t < GT; ++t) acc[t] = 0.0f;
+      [[maybe_unused]] f32x4 acc4 = {0.0f, 0.0f, 0.0f, 0.0f};
       // one key per lane: its row, 16 bytes at a time, against the sums in ascending d
       auto chunk = [&](auto cc) {
         constexpr int c = decltype(cc)::value;
         const v4u x = mine[lane * CH + (c ^ sw)];
         float kv[EPC];
         widen_chunk<ES>(x, kv);
+        if constexpr (kMatrix) {
+          int head = lane & 3;   // (opaque: the sums are read anew for every tile; kept, they would cost workgroups their places)
+          asm volatile("" : "+v"(head));
+          acc4 = mfma_chunk(acc4, sums + (hh + head) * SD + c * EPC, kv);
+          return;
+        }
 #pragma unroll
         for (int t = 0; t < GT; ++t) acc[t] = fma_chunk<(c * EPC) % 16, EPC>(acc[t], vq[t][(c * EPC) / 16], kv);
       };
       for_each_index(chunk, std::make_integer_sequence<int, CH>{});
+      if constexpr (kMatrix) {
+#pragma unroll
+        for (int t = 0; t < GT; ++t) acc[t] = acc4[t];
+      }
       if constexpr (ES == 1) {   // a power of two: exact, unless the product leaves the range of normal numbers
 #pragma unroll
         for (int t = 0; t < GT; ++t) acc[t] = acc[t] * scale_of(unit_now);
@@ -721,7 +757,7 @@ struct FusedLds {   // byte offsets inside the workgroup's dynamic LDS
   static constexpr size_t off_counts = off_a + size_t(GT) * kBinsA * 4;         // two bitmaps [GT][waves * tiles] of 64 bits, [2][waves] totals
   static constexpr size_t off_res = off_counts + size_t(GT) * kFusedWords * 16 + 2 * 8 * 4;   // [GT][4]
   static constexpr size_t off_sums = off_res + size_t(GT) * 16;                 // [GT][D]
-  static constexpr size_t bytes = off_sums + size_t(GT) * D * 4;
+  static constexpr size_t bytes = off_sums + size_t(GT) * kSumPitch<ES, D, GT> * 4;
 };
 
 // The bin that holds the kth-largest of the keys counted in hrow[0 .. NB) (bins descend from NB - 1), the
@@ -767,6 +803,8 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
   static_assert(NT <= 32, "a wave's tile masks are collected one per lane, its keys in one register vector per head");
   static_assert(GT <= W, "one wave scans one head's histogram");
   using Lds = FusedLds<ES, D, GT, NT>;
+  constexpr bool kMatrix = ES == 1 && GT == 4;
+  constexpr int SD = kSumPitch<ES, D, GT>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   v4u* mine_all = reinterpret_cast<v4u*>(lds);
   uint32_t* hist_b = reinterpret_cast<uint32_t*>(lds);            // [GT][kBinsB], once streaming is over
@@ -851,13 +889,13 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
         for (int j = 0; j < 32; ++j) a = a + x[j];
       }
       for (; i < nq; ++i) a = a + widen(p + i * qpitch);
-      sums[e] = a;
+      sums[e / D * SD + e % D] = a;
     }
     __syncthreads();
   }
   constexpr int NQ = D / 16;
-  float vq[GT][NQ];
-  {
+  float vq[kMatrix ? 1 : GT][NQ];
+  if constexpr (!kMatrix) {
     const float* qs = sums + (lane & 15);
 #pragma unroll
     for (int t = 0; t < GT; ++t)
@@ -885,15 +923,24 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
     float acc[GT];
 #pragma unroll
     for (int t = 0; t < GT; ++t) acc[t] = 0.0f;
+    [[maybe_unused]] f32x4 acc4 = {0.0f, 0.0f, 0.0f, 0.0f};
     auto chunk = [&](auto cc) {
       constexpr int c = decltype(cc)::value;
       const v4u x = mine[lane * CH + (c ^ sw)];
       float kv[EPC];
       widen_chunk<ES>(x, kv);
+      if constexpr (kMatrix) {
+        acc4 = mfma_chunk(acc4, sums + (lane & 3) * SD + c * EPC, kv);
+        return;
+      }
 #pragma unroll
       for (int t = 0; t < GT; ++t) acc[t] = fma_chunk<(c * EPC) % 16, EPC>(acc[t], vq[t][(c * EPC) / 16], kv);
     };
     for_each_index(chunk, std::make_integer_sequence<int, CH>{});
+    if constexpr (kMatrix) {
+#pragma unroll
+      for (int t = 0; t < GT; ++t) acc[t] = acc4[t];
+    }
     if constexpr (ES == 1) {
 #pragma unroll
       for (int t = 0; t < GT; ++t) acc[t] = acc[t] * scale_of(unit_now);
@@ -946,6 +993,10 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
     }
     __syncthreads();
     // (a wave with tiles has a full run before it; the wave after it may have none: its tiles then hold key 0)
+    // A wave's keys fall into few of the first histogram's bins, and its atomics on one word are served one after the other: where four
+    // heads of long lists are counted in the open, they go to four copies, in the cleared space of the later histograms (codes, 24
+    // sequences of 8192, 32 heads over 8 x 128, windows 3 / 5: 63.8 / 76.2 -> 61.7 / 72.6 us; no gain on lists of up to 1024).
+    constexpr bool kCopied = ES == 1 && GT == 4 && NT > kFusedTilesShort;
     const bool has_prev = wave > 0 && ntiles > 0, has_next = wave + 1 < W && ntiles > 0;
 #pragma unroll
     for (int t = 0; t < GT; ++t) {
@@ -986,10 +1037,23 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
       for (int u = 0; u < NT; ++u) {
         const bool valid = u < ntiles && first + u * 64 + lane < Lc;
         key[t][u] = valid ? best[u] : 0u;
-        if (valid) atomicAdd(&hist_a[t * kBinsA + (key[t][u] >> 22)], 1u);
+        if (valid) atomicAdd(&(kCopied ? hist_b + (lane & 3) * GT * kBinsA : hist_a)[t * kBinsA + (key[t][u] >> 22)], 1u);
       }
     }
     __syncthreads();
+    if constexpr (kCopied) {
+      for (int t = tid; t < GT * kBinsA; t += T) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          sum += hist_b[c * GT * kBinsA + t];
+          hist_b[c * GT * kBinsA + t] = 0;
+        }
+        hist_a[t] = sum;
+      }
+      static_assert(4 * kBinsA == 2 * kBinsB, "four copies fill the space");
+      __syncthreads();
+    }
   }
 
   // wave w < GT scans the histogram of head w and leaves {bin, rank, count} for all
@@ -1152,7 +1216,8 @@ static hipError_t launch_score(const Shape& s, const void* k, const void* q, con
   dim3 grid(s.hkv, (s.max_kv + rows_per_block - 1) / rows_per_block, s.batch);
   dim3 block(kScoreWaves * 64);
   const char *kp = static_cast<const char*>(k), *qp = static_cast<const char*>(q);
-  const size_t sums_bytes = size_t(s.group) * D * sizeof(float);   // dynamic LDS beside the 64 * 2*D-byte tiles
+  // dynamic LDS beside the 64 * 2*D-byte tiles
+  const size_t sums_bytes = size_t(s.group) * (s.group % 4 == 0 ? kSumPitch<ES, D, 4> : D) * sizeof(float);
   auto launch = [&](auto kernel) -> hipError_t {
     const hipError_t ea = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                               hipFuncAttributeMaxDynamicSharedMemorySize, int(sums_bytes));
