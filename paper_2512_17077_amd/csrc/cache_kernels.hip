@@ -63,10 +63,20 @@ __device__ __forceinline__ CacheJob cache_job(const Shape& s, const CacheView& c
   return j;
 }
 
+// Largest of x over the wave, the same in all lanes: the steps of wave_inclusive_sum, with the maximum (a lane without a source
+// adds zero, the least).
+template <int Ctrl, int RowMask>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
+  return max(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), Ctrl, RowMask, 0xf, false)));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) x = max(x, uint32_t(__shfl_xor(int(x), m)));
-  return x;
+  x = dpp_max<0x111, 0xf>(x);
+  x = dpp_max<0x112, 0xf>(x);
+  x = dpp_max<0x114, 0xf>(x);
+  x = dpp_max<0x118, 0xf>(x);
+  x = dpp_max<0x142, 0xa>(x);
+  x = dpp_max<0x143, 0xc>(x);
+  return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
 }
 // the larger of the two halves' magnitudes, kept in both halves of `most`
 __device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t most, uint32_t x) {
@@ -123,7 +133,7 @@ __global__ __launch_bounds__(kCacheWaves * 64) void cache_write_kernel(const cha
       else most = max(most, x[i][e] & 0x7fffffffu);
     }
   if constexpr (ES == 2) most = max(most << 16, most & 0xffff0000u);
-  most = __builtin_amdgcn_readfirstlane(int(wave_max(most)));
+  most = wave_max(most);
   const bool any = most > kMostStored;   // infinities, NaN or more than the format holds: one value at a time
   if (any) {
     most = 0;
@@ -135,7 +145,7 @@ __global__ __launch_bounds__(kCacheWaves * 64) void cache_write_kernel(const cha
         if (a < 0x7f800000u) most = max(most, a);
         if (ES == 2 && b < 0x7f800000u) most = max(most, b);
       }
-    most = __builtin_amdgcn_readfirstlane(int(wave_max(most)));
+    most = wave_max(most);
   }
   const uint32_t code = max(scale_byte(most), old);
   const float unit = scale_of(max(code, 1u));   // byte 0: zeros only

@@ -344,10 +344,10 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale:
     # a single head's row is as long as its scales say, whatever stride a tensor of one row has
     c.scale_stride_head = k_scale.stride(0) if k_scale.shape[0] > 1 else k_scale.shape[1]
     c.scale_block = int(scale_block)
-    # (not part of the C structure: the tensors stay alive with their descriptor; for the checks below)
+    # (not part of the C structure: the tensors stay alive with their descriptor, and what the checks of a call compare)
     c.tensors = (k, v, k_scale, v_scale)
-    c.shape = tuple(k.shape)
-    c.slots = int(k_scale.shape[1])
+    c.of = (int(k.shape[0]), int(k.shape[1]), int(k.shape[2]), k.device.index)
+    c.most_sequences = int(k_scale.shape[1]) - int(k.shape[0]) // c.scale_block
     return c
 
 
@@ -367,6 +367,7 @@ def make_cached_batch(q: torch.Tensor, cu_q: torch.Tensor, cu_kv: torch.Tensor, 
     b.max_q, b.max_kv = int(max_q), int(max_kv)
     b.softmax_scale = float(softmax_scale)
     b.tensors = (q, cu_q, cu_kv)   # (as in make_cache)
+    b.of, b.sequences = (b.total_kv, b.n_kv_heads, b.head_dim, q.device.index), b.batch
     return b
 
 
@@ -384,33 +385,40 @@ def make_rows_batch(k: torch.Tensor, v: torch.Tensor, cu_kv: torch.Tensor, total
     b.cu_kv = cu_kv.data_ptr()
     b.total_kv, b.max_kv = int(total_kv), int(max_kv)
     b.tensors = (k, v, cu_kv)   # (as in make_cache)
+    b.of, b.sequences = (b.total_kv, b.n_kv_heads, b.head_dim, k.device.index), b.batch
     b.rows = int(k.shape[0])
     return b
 
 
-def _check_cache(batch: DllmBatch, cache: DllmCache):
-    assert cache.shape == (batch.total_kv, batch.n_kv_heads, batch.head_dim), "the cache has another shape than the batch says"
-    assert cache.slots >= (batch.total_kv // cache.scale_block) + batch.batch, "too few scales (cache_scale_slots)"
+def _cached_stream(batch: DllmBatch, cache: DllmCache, stream) -> int:
+    """Checks that the two descriptors belong together and lie on the current device (where the call launches); the stream."""
+    assert batch.of == cache.of, "the cache has another shape or device than the batch says"
+    assert batch.sequences <= cache.most_sequences, "too few scales (cache_scale_slots)"
+    device = torch.cuda.current_device()
+    if device != cache.of[3]:
+        raise ValueError(f"the tensors are on device {cache.of[3]}, the current device is {device}")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _check_ranges(batch: DllmBatch, cu_rows, total_rows, at):
+def _rows_moved(batch: DllmBatch, cu_rows, total_rows: int, at) -> int:
+    """Rows of batch's tensors that a write or read moves, checked."""
     if cu_rows is None:
-        assert at is None and batch.rows >= batch.total_kv, "without cu_rows all rows are moved"
-        return batch.total_kv
-    assert cu_rows.dtype == torch.int32 and cu_rows.numel() == batch.batch + 1
-    assert at is None or (at.dtype == torch.int32 and at.numel() == batch.batch and at.is_contiguous())
-    assert batch.rows >= int(total_rows), "fewer rows than total_rows"
-    return int(total_rows)
+        assert at is None and batch.rows >= batch.of[0], "without cu_rows all rows are moved"
+        return batch.of[0]
+    assert cu_rows.dtype is torch.int32 and cu_rows.numel() == batch.sequences + 1
+    assert at is None or (at.dtype is torch.int32 and at.numel() == batch.sequences and at.is_contiguous())
+    assert batch.rows >= total_rows, "fewer rows than total_rows"
+    return total_rows
 
 
 def dllm_hcsa_cache_write(batch: DllmBatch, cache: DllmCache, cu_rows: Optional[torch.Tensor] = None, total_rows: int = 0,
                           max_rows: int = 0, at: Optional[torch.Tensor] = None, stream=None) -> DllmCache:
     """Quantise the rows of `batch` (make_rows_batch) into the cache: cu_rows[b] .. cu_rows[b+1]-1 to positions at[b] .. of
     sequence b (at None: its last ones), or every sequence whole (cu_rows None)."""
-    _check_cache(batch, cache)
-    total_rows = _check_ranges(batch, cu_rows, total_rows, at)
-    _raise(lib().dllm_hcsa_cache_write(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, int(max_rows),
-                                       _ptr(at), _stream(stream)))
+    total_rows = _rows_moved(batch, cu_rows, total_rows, at)
+    stream = _cached_stream(batch, cache, stream)
+    _raise(lib().dllm_hcsa_cache_write(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, max_rows, _ptr(at),
+                                       stream))
     return cache
 
 
@@ -418,11 +426,11 @@ def dllm_hcsa_cache_read(batch: DllmBatch, cache: DllmCache, k_out: torch.Tensor
                          cu_rows: Optional[torch.Tensor] = None, total_rows: int = 0, max_rows: int = 0,
                          at: Optional[torch.Tensor] = None, stream=None):
     """Read rows of the cache back into k_out / v_out, the tensors that `batch` describes (make_rows_batch)."""
-    _check_cache(batch, cache)
-    assert (k_out.data_ptr(), v_out.data_ptr()) == (batch.k or 0, batch.v or 0), "batch describes other tensors"
-    total_rows = _check_ranges(batch, cu_rows, total_rows, at)
-    _raise(lib().dllm_hcsa_cache_read(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, int(max_rows),
-                                      _ptr(at), _ptr(k_out), _ptr(v_out), _stream(stream)))
+    assert (batch.k or 0) == k_out.data_ptr() and (batch.v or 0) == v_out.data_ptr(), "batch describes other tensors"
+    total_rows = _rows_moved(batch, cu_rows, total_rows, at)
+    stream = _cached_stream(batch, cache, stream)
+    _raise(lib().dllm_hcsa_cache_read(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, max_rows, _ptr(at),
+                                      batch.k, batch.v, stream))
     return k_out, v_out
 
 
@@ -434,13 +442,13 @@ def dllm_hcsa_select_cached(batch: DllmBatch, cache: DllmCache, cu_k: torch.Tens
                             idx_out: torch.Tensor, pool_w: int = 1, forced_tail: int = 0, head_sum: bool = False,
                             workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Selection over the cached K (batch: make_cached_batch); fills idx_out [Hq, total_k] (int32, device)."""
-    _check_cache(batch, cache)
+    stream = _cached_stream(batch, cache, stream)
     if workspace is None:
         workspace = _workspace(dllm_hcsa_select_cached_workspace(batch, cache, max_k), idx_out.device)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_select_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_k), int(total_k), int(max_k),
                                          int(pool_w), int(forced_tail), int(bool(head_sum)), _ptr(idx_out), _ptr(workspace),
-                                         nbytes, _stream(stream)))
+                                         nbytes, stream))
     return idx_out
 
 
@@ -460,10 +468,10 @@ def dllm_hcsa_attend_cached_form_of(batch: DllmBatch, cache: DllmCache, lists: b
 def dllm_hcsa_attend_cached(batch: DllmBatch, cache: DllmCache, idx: Optional[torch.Tensor], cu_k: torch.Tensor, total_k: int,
                             max_k: int, o: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention over the cache: every head over its own list, or (idx None) all heads over the first rows of each sequence."""
-    _check_cache(batch, cache)
+    stream = _cached_stream(batch, cache, stream)
     if workspace is None:
         workspace = _workspace(dllm_hcsa_attend_cached_workspace(batch, cache, max_k), o.device)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_attend_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(idx), _ptr(cu_k), int(total_k),
-                                         int(max_k), _ptr(o), _ptr(workspace), nbytes, _stream(stream)))
+                                         int(max_k), _ptr(o), _ptr(workspace), nbytes, stream))
     return o

@@ -448,6 +448,11 @@ def test_attention_of_few_heads_over_long_sequences(hq, hkv, d, nq, lists):
     check_attend(filled(lens, hkv, d, 32, 71), hq, [nq] * 3, [4999, 1, 2111], 72, lists)
 
 
+@pytest.mark.parametrize("lists,keep", [(True, 100003), (False, 300001)])
+def test_attention_over_hundreds_of_thousands_of_rows(lists, keep):
+    check_attend(filled([300001], 1, 64, 64, 73), 2, [1], [keep], 74, lists)
+
+
 @pytest.mark.parametrize("lists", [True, False])
 def test_attention_of_batches_above_64_sequences(lists):
     lens = [int(n) for n in np.random.default_rng(2).integers(1, 200, 130)]
