@@ -5,14 +5,26 @@
 //            model, or a block over everything).  The query heads of a group then read the same rows, so a tile's 32
 //            columns are (query, head of the group) pairs of one KV head and the rows are read once per group.
 //
-// The step is bound by HBM, with half the bytes of the bf16 kernels (attend_sparse_bf16.hip), whose structure it keeps: a
-// workgroup of four waves walks one chunk of one list, each wave its own 32-row tiles without a workgroup barrier, and
-// what decides is how many rows are in flight.  A tile of codes takes half the registers of a bf16 tile, so a wave keeps
-// kDepth tiles ahead.  Codes are converted on their way from the registers to the wave's LDS tile: code * 2^e is a bf16
-// value exactly (one conversion instruction per two, which applies the scale too), so from there on the arithmetic is that
-// of a bf16 cache, and so is its precision: probabilities are rounded to bf16 for the product with V, outputs once at the end.
-// Scales are bytes, one per row of a tile and tensor: lane l fetches that of K row l % 32 (V: lanes 32 to 63) together with
-// the rows, and the lanes that convert a row get it by a lane exchange.
+// With scores z_ij = scale * q_i . k_j (in units of log 2) an output is sum_j 2^(z_ij - m_i) v_j / sum_j 2^(z_ij - m_i), in one pass
+// over the rows with the running maximum m_i and sum; parts of a list that different waves or workgroups have seen are joined by
+// weighting them with 2^(m_part - m).  A code times its scale is a bf16 value exactly, so the arithmetic is that of a bf16 cache:
+// probabilities are rounded to bf16 for the matrix cores (the sum adds the rounded ones, so that weights still sum to one), outputs once at the end.
+//
+// What bounds it: the rows, each read once (a block of 32 queries does 64 operations per byte of them, the matrix cores
+// could do 350 meanwhile).  Gathered rows of 128 bytes come at 4.0 TB/s at best, rows in order at 6.7; a
+// workgroup alone gets through a row of K and V in 7 ns, which decides where there are few lists.  So:
+//   - A workgroup of four waves walks one list or piece of one.  Each wave has a span of 32-row tiles of its own and LDS that
+//     no other wave touches, so the walk needs no workgroup barrier.
+//   - A tile's rows are fetched one tile ahead at head_dim 128, two at 64, into registers.  (Two ahead at 128: 24.6 us against 23.4 on sixteen
+//     ragged lists, 32 heads; the registers are better spent on operands.)
+//   - K goes into LDS as codes and is converted on its way into the matrix cores (half the LDS traffic of converting before);
+//     there a lane's 16 bytes are 16 elements of one row, and the queries, which stay in registers, are fetched in that
+//     order.  V, which is read transposed, 16 bits at a time, is converted first.  The conversion applies the scale.
+//   - Scales are bytes, one per tile row and tensor: lane l fetches that of K row l (V: row l - 32) with the tile.  K's are wanted
+//     by the lanes of that column in both halves (one exchange of halves), V's by the lane that converts the row (a lane exchange).
+//   - All of a tile's operands are asked for at once, V's before the softmax that stands between.
+// Measured (MI355X): sixteen lists of 5 to 50 % of 512 to 4096 positions, 32 heads x 128, 32 queries: 23.4 us; one layer of 32 heads,
+// 256 of 1024 positions: 7.0; single tokens of 32 sequences of 4000 to 8192, 32 heads over 8 x 128 (402 MB): 71.8, 5.6 TB/s.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -23,8 +35,6 @@ namespace dllm {
 
 constexpr int kWaves = 4;
 constexpr int kMaxListRows = 2048;   // kept rows of a list that one workgroup walks at most (their ids lie in LDS)
-
-typedef __attribute__((ext_vector_type(2))) __bf16 bf2;
 
 // 16 codes -> 16 bf16 values, in order
 __device__ __forceinline__ void widen_codes(v4u x, float unit, v4u& lo, v4u& hi) {
@@ -38,11 +48,9 @@ __device__ __forceinline__ void widen_codes(v4u x, float unit, v4u& lo, v4u& hi)
   hi = v4u{y[4], y[5], y[6], y[7]};
 }
 
-// Order of a row's 16-byte chunks of bf16 in an LDS tile: a lane converts 16 codes into two of them, and lays them half a row
-// apart, so that lanes side by side write chunks side by side (next to each other they would use every other bank only).  The queries
-// have the same order, so the sums over head_dim do not notice; outputs take it back.
-template <int D>
-__device__ __forceinline__ int place(int chunk) { return (chunk >> 1) + (chunk & 1) * (D / 16); }
+// A lane converts 16 codes of a V row into two 16-byte chunks of bf16 and lays them half a row apart, so that lanes side by side
+// write chunks side by side (next to each other they would use every other bank only).  The accumulators have that order, too: this is
+// the chunk of head_dim that stands at chunk `at` of a V tile's row.
 template <int D>
 __device__ __forceinline__ int placed(int at) { return at < D / 16 ? 2 * at : 2 * (at - D / 16) + 1; }
 
@@ -476,6 +484,7 @@ static int64_t pieces_per_head(const Shape& s, int64_t units) {
 //   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6), two on one unit 0.7 of their sum; the card reads gathered rows at
 //   4.9 TB/s, rows in order at 5.0, at 4.2 where every list is a workgroup's own (64-byte rows two thirds of that; all of it
 //   includes starting and draining).
+//   Without lists every column tile reads the rows again, from the caches: at 4.8 TB/s where lists are whole, 6.6 in pieces.
 //   Pieces cost a second launch and its latencies (3.3), what is written and read again (2.75 TB/s), and 1.4 for each further sequence that
 //   a piece reaches into.
 // One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 20.8 / 9.5; 32 of 4000 to 8192 78.9 / 73.2;
@@ -488,11 +497,12 @@ static bool better_in_pieces(const Shape& s, bool lists, int64_t heads, int64_t 
   const double read = double(total_k) * heads * 2 * s.d / (lists ? 4.9e6 : 5.0e6) * (s.d == 128 ? 1.0 : 1.5);
   double whole = max_k * row_us;
   if (units * s.batch > kUnits) whole = std::max(whole, total_k * units / kUnits * row_us * 0.7);
-  whole = std::max(whole, lists ? read : read * 1.2);
+  const bool again = !lists && tiles > 1;
+  whole = std::max(whole, again ? read * tiles * 5.0 / 4.8 : lists ? read : read * 1.2);
   double cut = piece * row_us;
   if (units * n > kUnits) cut *= s.d == 128 ? 1.4 : 1.3;
-  cut = std::max(cut, read) + 3.3 + 1.4 * (s.batch - 1) / n;
-  cut += (n + s.batch) * units * std::min<int64_t>(32, cols) * s.d * 8 / 2.75e6;
+  cut = std::max(cut, again ? read * tiles * 5.0 / 6.6 : read) + 3.3 + 1.4 * (s.batch - 1) / n;
+  cut += std::min(n + s.batch, 2 * n) * units * std::min<int64_t>(32, cols) * s.d * 8 / 2.75e6;
   return cut < whole;
 }
 static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, int64_t total_k) {
@@ -513,10 +523,13 @@ static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, i
     }
   }
   const int64_t wgs = heads * (p.piece ? p.n_pieces : s.batch);
-  p.groups = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles, 65535), resident / std::max<int64_t>(1, wgs)));
-  if (!p.piece && s.batch <= kRankBatch && p.groups == 1) {
-    if (wgs > resident) p.order = kLongestFirst;
-    else if (wgs > kUnits) p.order = kFolded;
+  // Where there are many column tiles, as many workgroups as fill the card four times share them out, so that units that get short
+  // lists take more of them: 32 heads x 128, 5 to 50 % of 500 to 4000 positions, once / four times, longest first: 8 sequences of 128 queries
+  // 53.4 / 42.6 us, of 256 101.7 / 77.3, 4 of 1024 182 / 136.
+  p.groups = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles, 65535), 4 * resident / std::max<int64_t>(1, wgs)));
+  if (!p.piece && s.batch <= kRankBatch) {
+    if (wgs * p.groups > resident) p.order = kLongestFirst;
+    else if (wgs > kUnits && p.groups == 1) p.order = kFolded;
   }
   return p;
 }

@@ -491,6 +491,17 @@ def test_attention_in_every_form(hq, hkv, d, batch, lo, hi, nq, pieces, lists):
 
 
 @pytest.mark.parametrize("lists", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,qlens,lens", [
+    (4, 4, 64, [300, 1, 0, 257], [90, 400, 33, 1]),                # several column tiles per workgroup or not, in one sequence
+    (8, 2, 128, [130, 64, 600], [500, 1200, 40]),                  # groups: four times the columns
+    (16, 4, 64, [40 + 13 * b for b in range(20)], [30 + 17 * b for b in range(20)]),   # longest first, column tiles apart
+    (2, 2, 64, [70] * 70, [60] * 70)])                             # more sequences than are ranked
+def test_attention_of_many_queries(hq, hkv, d, qlens, lens, lists):
+    """Blocks of many column tiles, of different lengths, which workgroups share out."""
+    check_attend(filled(lens, hkv, d, 16, 87), hq, qlens, [n - n // 3 for n in lens], 88, lists)
+
+
+@pytest.mark.parametrize("lists", [True, False])
 def test_large_scores_and_strided_queries(lists):
     c = filled([400, 333], 2, 128, 32, 91, layout="padded")
     wide = 8.0 * normal(40, 9, 136, torch.bfloat16, 92)
