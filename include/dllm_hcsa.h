@@ -274,6 +274,9 @@ dllm_status dllm_dense_refresh_attend(const dllm_batch *batch,
  * themselves or 2^-10 of the scale, whichever is more; larger ones are stored as 448 * 2^119, infinities and NaN as NaN (they
  * do not count for the scale).
  * Memory of a new cache must be zero where a part of a block may be written before the rest of it.
+ * Limits (DLLM_ERR_UNSUPPORTED beyond them): total_kv <= 2^31 - 129; a write or read moves fewer than 2^24 (block, four heads of K or V) pairs of
+ * one sequence; attention takes sequences of up to 2^24 tokens that span less than 4 GiB of codes, with stride_tok < 2^24, and
+ * lists of up to 2^27 - 2048 rows per head together.
  */
 typedef struct {
   uint8_t *k, *v;                  /* device, 16-byte aligned; codes of [total_kv, n_kv_heads, head_dim] */
@@ -334,9 +337,11 @@ dllm_status dllm_hcsa_select_cached(const dllm_batch *batch, const dllm_cache *c
  * o and must be DLLM_BF16; k, v and kv_stride_* of batch are not read.  With idx every head attends over its own list; with idx ==
  * NULL all heads of a sequence attend over its rows 0 .. k_b-1, which are then read once per KV head: for single tokens of an
  * autoregressive model (cu_kv gives every sequence's room, cu_k how much of it is filled) or a block over everything.  A
- * sequence with k_b == 0 gets zeros.  A query whose scores are NaN or overflow to plus infinity, or that attends over a NaN,
- * gets NaN; no other query's output changes.  A row that no query attends over may hold anything.
- * The workspace query serves calls with and without idx.
+ * sequence with k_b == 0 gets zeros.  A query whose scores are NaN, overflow to plus infinity or are all minus infinity, or that attends
+ * over a NaN, gets NaN; no other query's output changes.  A row that no query attends over may hold anything.
+ * The rows are read once per 32 queries (without lists: per 32 query-head pairs of a group), so for blocks of 128
+ * queries and more over everything dllm_hcsa_cache_read and dllm_dense_refresh_attend together take less time.
+ * The workspace query serves calls with and without idx; unless max_k or max_q is 0 it is never 0.
  */
 size_t dllm_hcsa_attend_cached_workspace(const dllm_batch *batch, const dllm_cache *cache, int32_t max_k);
 /*

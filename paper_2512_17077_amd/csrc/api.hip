@@ -584,8 +584,8 @@ dllm_status dllm_hcsa_attend_cached(const dllm_batch* batch, const dllm_cache* c
     return fail(DLLM_ERR_UNSUPPORTED,
                 "one sequence must have at most 2^24 rows spanning < 4 GiB with a token stride < 16 MiB (max_kv=%d, stride_tok=%lld)",
                 batch->max_kv, static_cast<long long>(view.tok));
-  if (idx != nullptr && total_k > (1 << 27))
-    return fail(DLLM_ERR_UNSUPPORTED, "lists of more than 2^27 rows per head together are not taken in one call (total_k=%d)", total_k);
+  if (idx != nullptr && total_k > (1 << 27) - 2048)   // (pieces of 2048 rows at most, and no more of them than a grid's y takes)
+    return fail(DLLM_ERR_UNSUPPORTED, "lists of more than 2^27 - 2048 rows per head together are not taken in one call (total_k=%d)", total_k);
   if ((st = check_workspace(workspace, workspace_bytes, dllm::attend_cached_workspace(s, max_k))) != DLLM_OK) return st;
   g_err[0] = 0;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);

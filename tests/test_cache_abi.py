@@ -177,6 +177,31 @@ def test_attend_cached_checks():
     assert attend(b, c) == UNSUPPORTED
 
 
+def test_the_largest_lists_that_attention_takes():
+    """Pieces of at most 2048 listed rows, at most 65535 of them; without lists the number of rows does not matter."""
+    b, c = good_batch(), good_cache()
+    most = (1 << 27) - 2048
+    assert (most + 2047) // 2048 == 65535
+    assert attend(b, c, total=most + 1) == UNSUPPORTED
+    assert attend(b, c, total=most, ws=None) == WORKSPACE   # the next check
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The calls launch on the current device."""
+    q, cu = torch.zeros((4, 2, 64), dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
+    codes, scales = torch.zeros((4, 2, 64), dtype=torch.uint8), torch.zeros((2, 2), dtype=torch.uint8)
+    c = hcsa.make_cache(codes, codes.clone(), scales, scales.clone(), 32)
+    b, rows = hcsa.make_cached_batch(q, cu, cu, 4, 2, 4, 4, 1.0), hcsa.make_rows_batch(q, q.clone(), cu, 4, 4)
+    c.of = b.of = rows.of = c.of[:3] + (1,)   # as if they lay on device 1
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="device 1.*device is 0"):
+        hcsa.dllm_hcsa_cache_write(rows, c)
+    with pytest.raises(ValueError, match="device 1"):
+        hcsa.dllm_hcsa_select_cached(b, c, cu, 4, 4, torch.zeros((2, 4), dtype=torch.int32))
+    with pytest.raises(ValueError, match="device 1"):
+        hcsa.dllm_hcsa_attend_cached(b, c, None, cu, 4, 4, q)
+
+
 def shaped(rng):
     b, c = good_batch(), good_cache()
     d, group = rng.choice((64, 128)), rng.choice((1, 2, 4, 5, 8))
