@@ -13,7 +13,7 @@
 // What bounds it: the rows, each read once (a block of 32 queries does 64 operations per byte of them, the matrix cores
 // could do 350 meanwhile).  Gathered rows of 128 bytes come at 4.0 TB/s at best, rows in order at 6.7; a
 // workgroup alone gets through a row of K and V in 7 ns, which decides where there are few lists.  So:
-//   - A workgroup of four waves walks one list or piece of one.  Each wave has a span of 32-row tiles of its own and LDS that
+//   - A workgroup of four waves walks one list or piece of one (or of four heads, see kSide).  Each wave has a span of 32-row tiles of its own and LDS that
 //     no other wave touches, so the walk needs no workgroup barrier.
 //   - A tile's rows are fetched one tile ahead at head_dim 128, two at 64, into registers.  (Two ahead at 128: 24.6 us against 23.4 on sixteen
 //     ragged lists, 32 heads; the registers are better spent on operands.)
@@ -24,7 +24,7 @@
 //     by the lanes of that column in both halves (one exchange of halves), V's by the lane that converts the row (a lane exchange).
 //   - All of a tile's operands are asked for at once, V's before the softmax that stands between.
 // Measured (MI355X): sixteen lists of 5 to 50 % of 512 to 4096 positions, 32 heads x 128, 32 queries: 23.4 us; one layer of 32 heads,
-// 256 of 1024 positions: 7.0; single tokens of 32 sequences of 4000 to 8192, 32 heads over 8 x 128 (402 MB): 71.8, 5.6 TB/s.
+// 256 of 1024 positions: 7.0; single tokens of 32 sequences of 4000 to 8192, 32 heads over 8 x 128 (379 MB): 67.2, 5.6 TB/s.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -88,10 +88,21 @@ __device__ __forceinline__ int sequence_at(const int32_t* __restrict__ cu_k, int
 enum : int { kAsTheyCome = 0, kLongestFirst = 1, kFolded = 2 };
 constexpr int kUnits = 256;   // compute units
 
+// Heads side by side (HW): in pieces without lists a workgroup's four waves can take a piece of four neighbouring KV heads, each wave one
+// of them and all of the piece, instead of a quarter of the piece of one head.  The rows of four heads lie side by side in memory, and
+// asked for together they come faster (reading alone, 8 heads x 128 codes: 6.7 TB/s against 5.6 to 6.0), and no merge of the
+// waves is left.  But a wave then has four times as many tiles one after the other.  8 heads x 128, single tokens, a head per workgroup /
+// four: 32 sequences of 4000 to 8192 72.8 / 67.2 us, 12 36.6 / 33.0, one of 8000 (pieces of 128, the least) 10.9 / 11.9; 4 heads, 8 of
+// 3000 to 8000 (160) 17.9 / 16.4; 16 heads x 64, 40 of 1000 to 5000 (896) 63.3 / 56.1, 4 x 64, 30 of 1000 to 8000 (288) 22.1 / 22.6.  So
+// from pieces of 160 rows on at head_dim 128, 512 at 64, and up to four column tiles (which read the rows again, from the caches: 24 sequences of 500
+// to 4000, 16 queries of 32 heads over 8, 53.4 / 49.7; 4 of 512 queries, 32 heads, 204 / 216).
+constexpr int kSide = 4;
+
 // Rows are shared out in pieces (Pieces): the lists of one head, laid end to end as cu_k has them, are cut every `piece` rows, and
 // a workgroup takes one piece of one head, whatever sequences it holds.  So all workgroups have the same work however long
 // the lists are, and those that a cut goes through are merged by a second launch.  Otherwise a workgroup takes one list whole.
-template <int D, bool Lists, bool Pieces>
+// HW: KV heads per workgroup (see kSide).
+template <int D, bool Lists, bool Pieces, int HW>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
     const uint16_t* __restrict__ q, CacheView c, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_kv,
     const int32_t* __restrict__ idx, const int32_t* __restrict__ cu_k, int32_t total_k, uint16_t* __restrict__ o,
@@ -104,6 +115,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
   constexpr int NDB = D / 32;
   constexpr int NT = D / 16;            // matrix-core steps along head_dim
   constexpr int W = kWaves;
+  constexpr int SP = W / HW;            // waves per head, each with a span of the rows
+  static_assert(W % HW == 0 && (HW == 1 || (Pieces && !Lists)), "heads side by side: in pieces without lists only");
   constexpr int MAXT = kMaxListRows / kTile / W;
   constexpr int kDepth = D == 128 ? 1 : 2;   // tiles in flight per wave
   constexpr int kMl = Lists ? MAXT * kTile : 64;
@@ -126,13 +139,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
       unit = int(2 * (pair % (n / 2)) + at / 8 % 2);
     }
   }
-  const int h0 = Lists ? unit : unit * s.group;   // first query head
-  const int g = Lists ? h0 / s.group : unit;
+  const int g = Lists ? unit / s.group : unit * HW + wave / SP;   // KV head of this wave
+  const int h0 = Lists ? unit : g * s.group;                      // its first query head
   const int heads = Lists ? 1 : s.group;
+  const int span = wave % SP;
   // column x of a sequence: query x / heads, head h0 + x % heads
   auto query_of = [&](int x) { return Lists ? x : int(uint32_t(x) / uint32_t(heads)); };
   auto clear = [&](int q0, int nq) {   // nothing kept: defined as zeros
-    for (int e = threadIdx.x; e < nq * heads * D; e += W * 64) {
+    for (int e = span * 64 + lane; e < nq * heads * D; e += SP * 64) {
       const int x = e / D, i = query_of(x);
       o[(int64_t(q0 + i) * s.hq + h0 + (x - i * heads)) * D + e % D] = 0;
     }
@@ -178,9 +192,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
       end = cu_k[s.batch];
       b = sequence_at(cu_k, s.batch, first, lane);
     }
-    if (px == 0 && blockIdx.z == 0)
-      for (int i = 0; i < s.batch; ++i)
-        if (cu_k[i + 1] == cu_k[i]) clear(cu_q[i], cu_q[i + 1] - cu_q[i]);
+    if (px == 0 && blockIdx.z == 0) {
+      if (small) {
+        for (uint64_t none = __builtin_amdgcn_ballot_w64(lane < s.batch && bi.kb == 0); none != 0; none &= none - 1) {
+          const int i = __builtin_ctzll(none);
+          clear(__builtin_amdgcn_readlane(bi.q0, i), __builtin_amdgcn_readlane(bi.nq, i));
+        }
+      } else {
+        for (int i = 0; i < s.batch; ++i)
+          if (cu_k[i + 1] == cu_k[i]) clear(cu_q[i], cu_q[i + 1] - cu_q[i]);
+      }
+    }
     if (first >= end) return;
     end = int(min(int64_t(first) + piece, int64_t(end)));
     enter(b);
@@ -220,7 +242,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
     const int c0 = sg.c0, c1 = sg.c1;
     const int ntiles = c1 > c0 ? (c1 - c0 + kTile - 1) / kTile : 0;
     // a wave's tiles are neighbours: it walks a span of its own
-    const int t0 = ntiles * wave / W, mine = ntiles * (wave + 1) / W - t0;
+    const int t0 = ntiles * span / SP, mine = ntiles * (span + 1) / SP - t0;
 
     for (int qt = blockIdx.z; ntiles > 0 && qt * 32 < ncols; qt += gridDim.z) {
       float m_used = -FLT_MAX, lsum = 0.0f;
@@ -331,64 +353,75 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
         }
       }
 
-      // ---- merge the waves' (m, l, O^T) through LDS that only they have used (as in attend_sparse_bf16_kernel)
+      // ---- what this wave's columns come to, merged over the waves of its head through LDS that only they have used
       const float l = sum_across_halves(lsum);
-      float* sm_ml = reinterpret_cast<float*>(&sm_rows[0][0]);   // [wave][m: 32 | l: 32], row stride kMl
-      if (hf == 0) {
-        sm_ml[wave * kMl + col] = m_used;
-        sm_ml[wave * kMl + 32 + col] = l;
-      }
-      float4* mrg = reinterpret_cast<float4*>(&lds[0][0]);
-      constexpr int kMrgWave = WAVEB / 16;
-      static_assert(NDB * 4 * 64 <= kMrgWave, "a wave's accumulators fit its tile buffers");
+      const int x = qt * 32 + col;
+      const int qi = query_of(x);
+      const int64_t row = int64_t(sg.q0 + qi) * s.hq + h0 + (x - qi * heads);
+      // elements 4 * u .. of the columns' output (u in the accumulators' order), times l_all
+      auto store = [&](int u, float4 a, float m_all, float l_all, float inv) {
+        const int at = placed<D>(u) * 8 + 4 * hf;
+        if (x >= ncols) return;
+        if (!Pieces || sg.parts == 1) {
+          *reinterpret_cast<v2u*>(o + row * D + at) = v2u{cvt_pk_bf16(a.x * inv, a.y * inv), cvt_pk_bf16(a.z * inv, a.w * inv)};
+        } else {
+          // (pieces and sequences only ever go up along a head's lists, so px + b numbers the segments)
+          const int64_t slot = (int64_t(px + sg.b) * s.max_q + qi) * s.hq + h0 + (x - qi * heads);
+          *reinterpret_cast<float4*>(po + slot * D + at) = a;
+          if (u == 0 && hf == 0) pml[slot] = make_float2(m_all, l_all);
+        }
+      };
+      if constexpr (SP == 1) {
+        const float inv = 1.0f / l;
 #pragma unroll
-      for (int db = 0; db < NDB; ++db)
+        for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4)
-          mrg[wave * kMrgWave + (db * 4 + i4) * 64 + lane] =
-              make_float4(acc[db][4 * i4 + 0], acc[db][4 * i4 + 1], acc[db][4 * i4 + 2], acc[db][4 * i4 + 3]);
-      __syncthreads();
-      {
-        constexpr int PARTS = W / NDB, NQ4 = 4 / PARTS;
-        static_assert(W % NDB == 0 && 4 % PARTS == 0, "the waves split the output evenly");
-        const int db = wave % NDB, i4_0 = (wave / NDB) * NQ4;
+          for (int i4 = 0; i4 < 4; ++i4)
+            store(db * 4 + i4, make_float4(acc[db][4 * i4 + 0], acc[db][4 * i4 + 1], acc[db][4 * i4 + 2], acc[db][4 * i4 + 3]),
+                  m_used, l, inv);
+      } else {
+        float* sm_ml = reinterpret_cast<float*>(&sm_rows[0][0]);   // [wave][m: 32 | l: 32], row stride kMl
+        if (hf == 0) {
+          sm_ml[wave * kMl + col] = m_used;
+          sm_ml[wave * kMl + 32 + col] = l;
+        }
+        float4* mrg = reinterpret_cast<float4*>(&lds[0][0]);
+        constexpr int kMrgWave = WAVEB / 16;
+        static_assert(NDB * 4 * 64 <= kMrgWave, "a wave's accumulators fit its tile buffers");
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4)
+            mrg[wave * kMrgWave + (db * 4 + i4) * 64 + lane] =
+                make_float4(acc[db][4 * i4 + 0], acc[db][4 * i4 + 1], acc[db][4 * i4 + 2], acc[db][4 * i4 + 3]);
+        __syncthreads();
+        constexpr int NU = NDB * 4 / SP;
+        static_assert(NDB * 4 % SP == 0, "the waves split the output evenly");
+        const int w0 = wave - span;
         float m_all = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < W; ++w) m_all = fmaxf(m_all, sm_ml[w * kMl + col]);
-        float f[W];
+        for (int w = 0; w < SP; ++w) m_all = fmaxf(m_all, sm_ml[(w0 + w) * kMl + col]);
+        float f[SP];
         float l_all = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-          f[w] = __builtin_amdgcn_exp2f(sm_ml[w * kMl + col] - m_all);   // 0 for a wave that saw no tile
-          l_all += sm_ml[w * kMl + 32 + col] * f[w];
+        for (int w = 0; w < SP; ++w) {
+          f[w] = __builtin_amdgcn_exp2f(sm_ml[(w0 + w) * kMl + col] - m_all);   // 0 for a wave that saw no tile
+          l_all += sm_ml[(w0 + w) * kMl + 32 + col] * f[w];
         }
-        const int x = qt * 32 + col;
-        const int qi = query_of(x);
-        const int64_t row = int64_t(sg.q0 + qi) * s.hq + h0 + (x - qi * heads);
         const float inv = 1.0f / l_all;
 #pragma unroll
-        for (int n = 0; n < NQ4; ++n) {
+        for (int n = 0; n < NU; ++n) {
+          const int u = span * NU + n;
           float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-          for (int w = 0; w < W; ++w) {
-            const float4 y = mrg[w * kMrgWave + (db * 4 + i4_0 + n) * 64 + lane];
+          for (int w = 0; w < SP; ++w) {
+            const float4 y = mrg[(w0 + w) * kMrgWave + u * 64 + lane];
             a.x += y.x * f[w]; a.y += y.y * f[w]; a.z += y.z * f[w]; a.w += y.w * f[w];
           }
-          const int at = placed<D>(db * 4 + i4_0 + n) * 8 + 4 * hf;
-          if (x < ncols) {
-            if (!Pieces || sg.parts == 1) {
-              *reinterpret_cast<v2u*>(o + row * D + at) =
-                  v2u{cvt_pk_bf16(a.x * inv, a.y * inv), cvt_pk_bf16(a.z * inv, a.w * inv)};
-            } else {
-              // (pieces and sequences only ever go up along a head's lists, so px + b numbers the segments)
-              const int64_t slot = (int64_t(px + sg.b) * s.max_q + qi) * s.hq + h0 + (x - qi * heads);
-              *reinterpret_cast<float4*>(po + slot * D + at) = a;
-              if (n == 0 && wave == 0 && hf == 0) pml[slot] = make_float2(m_all, l_all);
-            }
-          }
+          store(u, a, m_all, l_all, inv);
         }
+        __syncthreads();   // merge space becomes tile space again
       }
-      __syncthreads();   // merge space becomes tile space again
     }
     if constexpr (!Pieces) break;
     else {
@@ -473,6 +506,7 @@ __global__ __launch_bounds__(256) void merge_pieces_kernel(const int32_t* __rest
 // How a call's rows are shared out: in pieces of `piece` rows, or (0) a list per workgroup.
 struct CachePlan {
   int32_t piece, n_pieces;   // per head
+  int32_t side;              // KV heads per workgroup
   int64_t groups;            // workgroups that share the column tiles of a sequence
   int order;
 };
@@ -482,27 +516,26 @@ static int64_t pieces_per_head(const Shape& s, int64_t units) {
 }
 // Lists whole or in pieces: the less of two sums, in us, from these measurements.
 //   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6), two on one unit 0.7 of their sum; the card reads gathered rows at
-//   4.9 TB/s, rows in order at 5.0, at 4.2 where every list is a workgroup's own (64-byte rows two thirds of that; all of it
+//   4.9 TB/s, rows in order at 5.0, at 6.2 with heads side by side, at 4.2 where every list is a workgroup's own (64-byte rows two thirds of that; all of it
 //   includes starting and draining).
-//   Without lists every column tile reads the rows again, from the caches: at 4.8 TB/s where lists are whole, 6.6 in pieces.
-//   Pieces cost a second launch and its latencies (3.3), what is written and read again (2.75 TB/s), and 1.4 for each further sequence that
+//   Without lists every column tile reads the rows again, from the caches, in pieces at 6.6 TB/s.
+//   Pieces cost a second launch and its latencies (3.3), what is written and read again (2.75 TB/s, without lists 3.5), and 1.4 for each further sequence that
 //   a piece reaches into.
-// One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 20.8 / 9.5; 32 of 4000 to 8192 78.9 / 73.2;
-// 16 of 1000 13.5 / 16.1; 40 of 100 to 1000 19.8 / 23.3; lists of 32 heads x 128, one of 4096 rows 25.9 / 14.5, of 512 9.2 / 9.5, of 256 7.0 / 9.7; four
-// of 276 to 994 12.8 / 16.9; sixteen of 5 to 50 % of 512 to 4096 28.9 / 36.3.  Over 640 batches, 1 to 40 sequences of 128 to 8192, the
-// choice is 0.3 % above the better one in the mean, 37 % at most (one list of 1021 rows over 32 heads).
+// One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 20.8 / 9.5; 32 of 4000 to 8192 79.2 / 67.2;
+// 16 of 1000 13.5 / 16.1; 40 of 100 to 1000 16.1 / 19.4; lists of 32 heads x 128, one of 4096 rows 25.9 / 14.5, of 512 9.2 / 9.5, of 256 7.0 / 9.7; four
+// of 276 to 994 12.8 / 16.9; sixteen of 5 to 50 % of 512 to 4096 28.9 / 36.3.  Over 350 batches, 1 to 40 sequences of 128 to 8192, the
+// choice is 0.3 % above the better one in the mean, 22 % at most (single tokens of ten sequences of 74 to 163 over 16 heads x 64, 6.1 against 7.5).
 static bool better_in_pieces(const Shape& s, bool lists, int64_t heads, int64_t cols, int64_t tiles, int64_t max_k, int64_t total_k,
-                             int64_t piece) {
+                             int64_t piece, int64_t side) {
   const double row_us = s.d == 128 ? 7.0e-3 : 4.6e-3, units = double(heads * tiles), n = double((total_k + piece - 1) / piece);
   const double read = double(total_k) * heads * 2 * s.d / (lists ? 4.9e6 : 5.0e6) * (s.d == 128 ? 1.0 : 1.5);
   double whole = max_k * row_us;
   if (units * s.batch > kUnits) whole = std::max(whole, total_k * units / kUnits * row_us * 0.7);
-  const bool again = !lists && tiles > 1;
-  whole = std::max(whole, again ? read * tiles * 5.0 / 4.8 : lists ? read : read * 1.2);
-  double cut = piece * row_us;
-  if (units * n > kUnits) cut *= s.d == 128 ? 1.4 : 1.3;
-  cut = std::max(cut, again ? read * tiles * 5.0 / 6.6 : read) + 3.3 + 1.4 * (s.batch - 1) / n;
-  cut += std::min(n + s.batch, 2 * n) * units * std::min<int64_t>(32, cols) * s.d * 8 / 2.75e6;
+  whole = std::max(whole, lists ? read : read * 1.2 * tiles);
+  double cut = piece * side * row_us;
+  if (units / side * n > kUnits) cut *= s.d == 128 ? 1.4 : 1.3;
+  cut = std::max(cut, !lists && tiles > 1 ? read * tiles * 5.0 / 6.6 : side > 1 ? read * 5.0 / 6.2 : read) + 3.3 + 1.4 * (s.batch - 1) / n;
+  cut += std::min(n + s.batch, 2 * n) * units * std::min<int64_t>(32, cols) * s.d * 8 / (lists ? 2.75e6 : 3.5e6);
   return cut < whole;
 }
 static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, int64_t total_k) {
@@ -510,19 +543,28 @@ static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, i
   total_k = std::min<int64_t>(total_k, int64_t(s.batch) * max_k);
   const int64_t heads = lists ? s.hq : s.hkv, cols = lists ? s.max_q : int64_t(s.max_q) * s.group;
   const int64_t tiles = std::max<int64_t>(1, (cols + 31) / 32), units = heads * tiles, resident = 2 * kUnits;
+  p.side = 1;
   if (max_k > 0) {
-    const int64_t share = (total_k + pieces_per_head(s, units) - 1) / pieces_per_head(s, units);
-    int64_t piece = std::max<int64_t>(128, (share + 31) / 32 * 32);
+    auto piece_for = [&](int64_t side) {
+      const int64_t n = pieces_per_head(s, units / side), share = (total_k + n - 1) / n;
+      return std::max<int64_t>(128, (share + 31) / 32 * 32);
+    };
+    int64_t piece = piece_for(1);
+    if (!lists && s.hkv % kSide == 0 && tiles <= 4 && piece_for(kSide) >= (s.d == 128 ? 160 : 512)) {
+      p.side = kSide;
+      piece = piece_for(kSide);
+    }
     // (the ids of a list's rows lie in LDS: no workgroup takes more than kMaxListRows of them, whole or in pieces)
     bool cut = lists && max_k > kMaxListRows;
-    if (!cut && !(lists && piece > kMaxListRows)) cut = better_in_pieces(s, lists, heads, cols, tiles, max_k, total_k, piece);
+    if (!cut && !(lists && piece > kMaxListRows))
+      cut = better_in_pieces(s, lists, heads, cols, tiles, max_k, total_k, piece, p.side);
     if (lists) piece = std::min<int64_t>(piece, kMaxListRows);
     if (cut) {
       p.piece = int32_t(std::min<int64_t>(piece, INT32_MAX));
       p.n_pieces = int32_t((total_k + p.piece - 1) / p.piece);
     }
   }
-  const int64_t wgs = heads * (p.piece ? p.n_pieces : s.batch);
+  const int64_t wgs = p.piece ? heads / p.side * p.n_pieces : heads * s.batch;
   // Where there are many column tiles, as many workgroups as fill the card four times share them out, so that units that get short
   // lists take more of them: 32 heads x 128, 5 to 50 % of 500 to 4000 positions, once / four times, longest first: 8 sequences of 128 queries
   // 53.4 / 42.6 us, of 256 101.7 / 77.3, 4 of 1024 182 / 136.
@@ -543,7 +585,8 @@ static size_t partial_slots(const Shape& s, int64_t n_pieces) {
 size_t attend_cached_workspace(const Shape& s, int32_t max_k) {
   if (max_k == 0 || s.max_q == 0) return 0;
   const int64_t tiles = (int64_t(s.max_q) + 31) / 32, group_tiles = (int64_t(s.max_q) * s.group + 31) / 32;
-  int64_t n = std::max(pieces_per_head(s, s.hq * tiles), pieces_per_head(s, s.hkv * group_tiles));
+  const int64_t side = s.hkv % kSide == 0 && group_tiles <= 4 ? kSide : 1;
+  int64_t n = std::max(pieces_per_head(s, s.hq * tiles), pieces_per_head(s, s.hkv / side * group_tiles));
   if (max_k > kMaxListRows) n = std::max<int64_t>(n, (int64_t(s.batch) * max_k + kMaxListRows - 1) / kMaxListRows);
   const size_t slots = partial_slots(s, n);
   return align256(slots * s.d * sizeof(float)) + align256(slots * sizeof(float2));
@@ -560,7 +603,7 @@ hipError_t launch_attend_cached(const Shape& s, const CacheView& c, int32_t max_
   const uint16_t* qh = static_cast<const uint16_t*>(q);
   uint16_t* oh = static_cast<uint16_t*>(o);
   // Without lists the heads of one piece run on one XCD if the number of pieces is a multiple of eight: their rows lie side by side.
-  const unsigned heads = lists ? s.hq : s.hkv;
+  const unsigned heads = lists ? s.hq : p.piece ? s.hkv / p.side : s.hkv;
   const unsigned parts = !p.piece ? s.batch : lists || p.n_pieces < 8 ? p.n_pieces : (p.n_pieces + 7) / 8 * 8;
   auto launch = [&](auto kernel, bool heads_first) {
     const dim3 grid(heads_first ? heads : parts, heads_first ? parts : heads, unsigned(p.groups));
@@ -569,11 +612,12 @@ hipError_t launch_attend_cached(const Shape& s, const CacheView& c, int32_t max_
   auto with_d = [&](auto d) {
     constexpr int D = decltype(d)::value;
     if (p.piece) {
-      if (lists) launch(attend_cache_kernel<D, true, true>, true);
-      else launch(attend_cache_kernel<D, false, true>, false);
+      if (lists) launch(attend_cache_kernel<D, true, true, 1>, true);
+      else if (p.side == kSide) launch(attend_cache_kernel<D, false, true, kSide>, false);
+      else launch(attend_cache_kernel<D, false, true, 1>, false);
     } else {
-      if (lists) launch(attend_cache_kernel<D, true, false>, true);
-      else launch(attend_cache_kernel<D, false, false>, true);
+      if (lists) launch(attend_cache_kernel<D, true, false, 1>, true);
+      else launch(attend_cache_kernel<D, false, false, 1>, true);
     }
   };
   if (s.d == 128) with_d(std::integral_constant<int, 128>{});

@@ -490,6 +490,22 @@ def test_attention_in_every_form(hq, hkv, d, batch, lo, hi, nq, pieces, lists):
     check_attend(c, hq, [nq] * batch, keep, 86, lists)
 
 
+@pytest.mark.parametrize("hq,hkv,d,nq,lens", [
+    (8, 8, 128, 1, [9001, 1, 0, 7003, 4000, 33]),       # single tokens; sequences that a piece holds whole
+    (8, 4, 128, 60, [5003, 2, 3000, 0, 1700]),          # several column tiles
+    (16, 4, 64, 31, [40001, 25000, 1, 3333]),
+    (12, 12, 128, 2, [20 * (b % 7) for b in range(89)] + [14000])])   # more sequences than a wave holds
+def test_attention_of_heads_side_by_side(hq, hkv, d, nq, lens):
+    """Without lists, in pieces long enough that a workgroup takes four KV heads."""
+    c = filled(lens, hkv, d, 32, 89)
+    keep = [n - n // 50 for n in lens]
+    b = hcsa.make_cached_batch(torch.zeros((nq * len(lens), hq, d), dtype=torch.bfloat16, device=DEV), c.cu_t, c.cu_t, c.total, hkv, nq, max(lens), 1)
+    pieces = (256 if d == 128 else 512) // (hkv // 4 * ((nq * (hq // hkv) + 31) // 32))
+    piece = (-(-sum(keep) // pieces) + 31) // 32 * 32
+    assert hcsa.dllm_hcsa_attend_cached_form_of(b, c.desc, False, max(keep), sum(keep)) == piece >= (160 if d == 128 else 512)
+    check_attend(c, hq, [nq] * len(lens), keep, 90, False)
+
+
 @pytest.mark.parametrize("lists", [True, False])
 @pytest.mark.parametrize("hq,hkv,d,qlens,lens", [
     (4, 4, 64, [300, 1, 0, 257], [90, 400, 33, 1]),                # several column tiles per workgroup or not, in one sequence
