@@ -24,7 +24,7 @@
 //     by the lanes of that column in both halves (one exchange of halves), V's by the lane that converts the row (a lane exchange).
 //   - All of a tile's operands are asked for at once, V's before the softmax that stands between.
 // Measured (MI355X): sixteen lists of 5 to 50 % of 512 to 4096 positions, 32 heads x 128, 32 queries: 23.4 us; one layer of 32 heads,
-// 256 of 1024 positions: 7.0; single tokens of 32 sequences of 4000 to 8192, 32 heads over 8 x 128 (379 MB): 67.2, 5.6 TB/s.
+// 256 of 1024 positions: 5.8; single tokens of 32 sequences of 4000 to 8192, 32 heads over 8 x 128 (379 MB): 67.2, 5.6 TB/s.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -102,7 +102,7 @@ constexpr int kSide = 4;
 // a workgroup takes one piece of one head, whatever sequences it holds.  So all workgroups have the same work however long
 // the lists are, and those that a cut goes through are merged by a second launch.  Otherwise a workgroup takes one list whole.
 // HW: KV heads per workgroup (see kSide).
-template <int D, bool Lists, bool Pieces, int HW>
+template <int D, bool Lists, bool Pieces, int HW, int VS>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
     const uint16_t* __restrict__ q, CacheView c, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_kv,
     const int32_t* __restrict__ idx, const int32_t* __restrict__ cu_k, int32_t total_k, uint16_t* __restrict__ o,
@@ -110,9 +110,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
     Shape s DLLM_CHECK_PARAM) {
   DLLM_CHECK_EXIT();
   constexpr int CC = D / 16;            // 16-byte chunks of a row of codes
-  constexpr int KTILEB = kTile * D, VTILEB = kTile * 2 * D;   // K lies in LDS as codes, V as bf16
-  constexpr int NLD = kTile * CC / 64;  // 16-byte loads per lane, tile and tensor
-  constexpr int NDB = D / 32;
+  constexpr int DV = D / VS, CV = CC / VS;   // elements and 16-byte chunks of a V row that this workgroup takes
+  constexpr int KTILEB = kTile * D, VTILEB = kTile * 2 * DV;   // K lies in LDS as codes, V as bf16
+  constexpr int NLD = kTile * CC / 64;  // 16-byte loads of K per lane and tile
+  constexpr int NLV = NLD / VS;         // ... of V
+  constexpr int NDB = DV / 32;
   constexpr int NT = D / 16;            // matrix-core steps along head_dim
   constexpr int W = kWaves;
   constexpr int SP = W / HW;            // waves per head, each with a span of the rows
@@ -143,6 +145,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
   const int h0 = Lists ? unit : g * s.group;                      // its first query head
   const int heads = Lists ? 1 : s.group;
   const int span = wave % SP;
+  // VS: workgroups that share a list's columns of V, where there are units to spare.  One unit gets 36 GB/s of gathered rows, with eight
+  // waves no more than with four, so that each takes all of K and its part of V, and needs no merge: lists of 256 / 512 / 1024 rows,
+  // 32 heads x 128, alone 7.14 / 9.45 / 14.1 us, in four 5.72 / 7.22 / 10.7; four of 276 to 994 in two 13.0 -> 11.3; single tokens of two
+  // sequences of 847 and 738, 8 KV heads, in four 12.1 -> 8.7.  (Two workgroups per unit: 11.3 -> 17.3.)
+  const int part = VS > 1 ? int(blockIdx.z) % VS : 0;   // of V's columns
+  const int qt0 = VS > 1 ? int(blockIdx.z) / VS : blockIdx.z, qt_step = gridDim.z / VS;   // column tiles
   // column x of a sequence: query x / heads, head h0 + x % heads
   auto query_of = [&](int x) { return Lists ? x : int(uint32_t(x) / uint32_t(heads)); };
   auto clear = [&](int q0, int nq) {   // nothing kept: defined as zeros
@@ -214,7 +222,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
     }
     const SeqInfo si = sequence_of_slot(cu_q, cu_kv, cu_k, s.batch, place_of, lane, order != kAsTheyCome);
     if (si.kb == 0) {
-      if (blockIdx.z == 0) clear(si.q0, si.nq);
+      if (qt0 == 0 && part == 0) clear(si.q0, si.nq);
       return;
     }
     sg = {si.b, si.ko0, si.kb, 0, Lists ? min(si.kb, kMaxListRows) : si.kb, 1, si.q0, si.nq, si.kv0};
@@ -223,9 +231,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
   char* ktile = lds[wave];
   char* vtile = lds[wave] + KTILEB;
   const int koff = codes_off<D>(col, hf);   // K operand: chunks 2u + hf of row col
-  VtAddr<D> vt;
+  VtAddr<DV> vt;
   vt.init(lane);
   const uint32_t coff = uint32_t(lane) % CC * 16;
+  const uint32_t voff = uint32_t(lane) % CV * 16 + part * DV;
   const uint32_t pitch = uint32_t(c.tok);   // a sequence's rows span < 4 GiB (checked on the host)
   const float zscale = s.scale * kLog2e;
   auto opaque = [](int x) {
@@ -244,7 +253,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
     // a wave's tiles are neighbours: it walks a span of its own
     const int t0 = ntiles * span / SP, mine = ntiles * (span + 1) / SP - t0;
 
-    for (int qt = blockIdx.z; ntiles > 0 && qt * 32 < ncols; qt += gridDim.z) {
+    for (int qt = qt0; ntiles > 0 && qt * 32 < ncols; qt += qt_step) {
       float m_used = -FLT_MAX, lsum = 0.0f;
       f32x16 acc[NDB];
 #pragma unroll
@@ -275,20 +284,25 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 
-      v4u kr[kDepth][NLD], vr[kDepth][NLD];
+      v4u kr[kDepth][NLD], vr[kDepth][NLV];
       uint32_t sc[kDepth];
       // row `r` (0 .. 31) of the wave's j-th tile
       auto row_of = [&](int j, int r) {
         return Lists ? my_rows[j * kTile + r] : min(c0 + (t0 + j) * kTile + r, c1 - 1);
       };
-      auto fetch = [&](v4u (&kx)[NLD], v4u (&vx)[NLD], uint32_t& sx, int j) {
+      auto fetch = [&](v4u (&kx)[NLD], v4u (&vx)[NLV], uint32_t& sx, int j) {
         const uint32_t lane_o = opaque(lane);
         sx = sbase[uint32_t(row_of(j, lane_o & 31)) >> c.shift];
 #pragma unroll
         for (int i = 0; i < NLD; ++i) {
           const uint32_t off = __umul24(uint32_t(row_of(j, (i * 64 + lane_o) / CC)), pitch) + coff;
           kx[i] = load_once(kbase + off);
-          vx[i] = load_once(vbase + off);
+          if constexpr (VS == 1) vx[i] = load_once(vbase + off);
+        }
+        if constexpr (VS > 1) {
+#pragma unroll
+          for (int i = 0; i < NLV; ++i)
+            vx[i] = load_once(vbase + __umul24(uint32_t(row_of(j, (i * 64 + lane_o) / CV)), pitch) + voff);
         }
       };
 #pragma unroll
@@ -299,7 +313,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
         for (int d = 0; d < kDepth; ++d) {
           const int j = j0 + d, tile = t0 + j;
           if (j < mine) {
-            VtAddr<D> vtr;
+            VtAddr<DV> vtr;
             vtr.base[0] = opaque(vt.base[0]);
             vtr.base[1] = opaque(vt.base[1]);
             const uint32_t lane_o = opaque(lane);
@@ -307,13 +321,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
             const float ku = scale_of(both[0]);   // of K row col, in both halves
 #pragma unroll
             for (int i = 0; i < NLD; ++i) {
-              const uint32_t f = i * 64 + lane_o, r = f / CC, cc = f % CC;
+              const uint32_t f = i * 64 + lane_o;
+              *reinterpret_cast<v4u*>(ktile + codes_off<D>(f / CC, f % CC)) = kr[d][i];
+              if (i >= NLV) continue;
+              const uint32_t r = f / CV, cc = f % CV;
               const float vu = scale_of(uint32_t(__builtin_amdgcn_ds_bpermute(int(r * 4 + 128), int(sc[d]))));
-              *reinterpret_cast<v4u*>(ktile + codes_off<D>(r, cc)) = kr[d][i];
               v4u lo, hi;
               widen_codes(vr[d][i], vu, lo, hi);
-              *reinterpret_cast<v4u*>(vtile + tile_off<D>(r, cc)) = lo;
-              *reinterpret_cast<v4u*>(vtile + tile_off<D>(r, cc + CC)) = hi;
+              *reinterpret_cast<v4u*>(vtile + tile_off<DV>(r, cc)) = lo;
+              *reinterpret_cast<v4u*>(vtile + tile_off<DV>(r, cc + CV)) = hi;
             }
             if (j + kDepth < mine) fetch(kr[d], vr[d], sc[d], j + kDepth);
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -328,8 +344,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
             for (int u = 0; u < 2; ++u)
 #pragma unroll
               for (int db = 0; db < NDB; ++db) {
-                const v2u lo = lds_read_tr16(vtile + vtr.off(0, db) + 16 * u * 2 * D);
-                const v2u hi = lds_read_tr16(vtile + vtr.off(1, db) + 16 * u * 2 * D);
+                const v2u lo = lds_read_tr16(vtile + vtr.off(0, db) + 16 * u * 2 * DV);
+                const v2u hi = lds_read_tr16(vtile + vtr.off(1, db) + 16 * u * 2 * DV);
                 vx[u][db] = v4u{lo.x, lo.y, hi.x, hi.y};
               }
             f32x16 st;
@@ -360,7 +376,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
       const int64_t row = int64_t(sg.q0 + qi) * s.hq + h0 + (x - qi * heads);
       // elements 4 * u .. of the columns' output (u in the accumulators' order), times l_all
       auto store = [&](int u, float4 a, float m_all, float l_all, float inv) {
-        const int at = placed<D>(u) * 8 + 4 * hf;
+        const int at = part * DV + placed<DV>(u) * 8 + 4 * hf;
         if (x >= ncols) return;
         if (!Pieces || sg.parts == 1) {
           *reinterpret_cast<v2u*>(o + row * D + at) = v2u{cvt_pk_bf16(a.x * inv, a.y * inv), cvt_pk_bf16(a.z * inv, a.w * inv)};
@@ -507,6 +523,7 @@ __global__ __launch_bounds__(256) void merge_pieces_kernel(const int32_t* __rest
 struct CachePlan {
   int32_t piece, n_pieces;   // per head
   int32_t side;              // KV heads per workgroup
+  int32_t v_split;           // workgroups that share the columns of V
   int64_t groups;            // workgroups that share the column tiles of a sequence
   int order;
 };
@@ -515,34 +532,49 @@ static int64_t pieces_per_head(const Shape& s, int64_t units) {
   return std::max<int64_t>(1, (s.d == 128 ? kUnits : 2 * kUnits) / units);
 }
 // Lists whole or in pieces: the less of two sums, in us, from these measurements.
-//   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6), two on one unit 0.7 of their sum; the card reads gathered rows at
-//   4.9 TB/s, rows in order at 5.0, at 6.2 with heads side by side, at 4.2 where every list is a workgroup's own (64-byte rows two thirds of that; all of it
-//   includes starting and draining).
+//   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6, whole lists in order 6.0; with half of V 0.78 of that, with a
+//   quarter 0.72), two on one unit 0.7 of their sum; where there are more than two, every one takes 4.5 us beside its rows.
+//   The card reads gathered rows at 4.9 TB/s, rows in order at 5.0, at 6.2 with heads side by side, at 4.2 where every list is a
+//   workgroup's own (3.5 where two share V's columns; 64-byte rows two thirds of all that; it includes starting and draining).
 //   Without lists every column tile reads the rows again, from the caches, in pieces at 6.6 TB/s.
-//   Pieces cost a second launch and its latencies (3.3), what is written and read again (2.75 TB/s, without lists 3.5), and 1.4 for each further sequence that
-//   a piece reaches into.
-// One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 20.8 / 9.5; 32 of 4000 to 8192 79.2 / 67.2;
-// 16 of 1000 13.5 / 16.1; 40 of 100 to 1000 16.1 / 19.4; lists of 32 heads x 128, one of 4096 rows 25.9 / 14.5, of 512 9.2 / 9.5, of 256 7.0 / 9.7; four
-// of 276 to 994 12.8 / 16.9; sixteen of 5 to 50 % of 512 to 4096 28.9 / 36.3.  Over 350 batches, 1 to 40 sequences of 128 to 8192, the
-// choice is 0.3 % above the better one in the mean, 22 % at most (single tokens of ten sequences of 74 to 163 over 16 heads x 64, 6.1 against 7.5).
+//   Pieces cost a second launch and its latencies (3.3), what is written and read again (2.75 TB/s, without lists 3.5), and for the further
+//   sequences that a piece reaches into 1.4 each with lists, in the mean, 2.5 without, in the piece that has most.
+// One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 15.5 / 9.4; 32 of 4000 to 8192 79.2 / 67.2;
+// 16 of 1000 12.2 / 17.4; 40 of 100 to 1000 16.1 / 19.4; lists of 32 heads x 128, one of 4096 rows 25.9 / 14.5, of 1024 10.7 / 10.0, of 256 5.7 / 9.5; four
+// of 276 to 994 11.3 / 16.9; sixteen of 5 to 50 % of 512 to 4096 23.3 / 36.3.  Over 700 batches, 1 to 40 sequences of 128 to 8192, the
+// choice is 0.3 % above the better one in the mean, 43 % at most (single tokens of 25 sequences of 3440, 4 heads x 64, 25.7 against 18.0).
 static bool better_in_pieces(const Shape& s, bool lists, int64_t heads, int64_t cols, int64_t tiles, int64_t max_k, int64_t total_k,
-                             int64_t piece, int64_t side) {
+                             int64_t piece, int64_t side, int32_t v_split) {
   const double row_us = s.d == 128 ? 7.0e-3 : 4.6e-3, units = double(heads * tiles), n = double((total_k + piece - 1) / piece);
   const double read = double(total_k) * heads * 2 * s.d / (lists ? 4.9e6 : 5.0e6) * (s.d == 128 ? 1.0 : 1.5);
-  double whole = max_k * row_us;
-  if (units * s.batch > kUnits) whole = std::max(whole, total_k * units / kUnits * row_us * 0.7);
-  whole = std::max(whole, lists ? read : read * 1.2 * tiles);
+  const double whole_row_us = lists || s.d == 128 ? row_us : 6.0e-3, wgs = units * s.batch;
+  double whole = max_k * whole_row_us * (v_split == 4 ? 0.72 : v_split == 2 ? 0.78 : 1.0);
+  if (wgs > kUnits) whole = std::max(whole, total_k * units / kUnits * row_us * 0.7);
+  whole = std::max(whole, lists ? read : read * 1.2 * tiles * (v_split == 2 ? 1.2 : 1.0));
+  if (!lists && wgs > 2 * kUnits) whole = std::max(whole, wgs / (2 * kUnits) * (4.5 + double(total_k) / s.batch * row_us * 1.4));
   double cut = piece * side * row_us;
   if (units / side * n > kUnits) cut *= s.d == 128 ? 1.4 : 1.3;
-  cut = std::max(cut, !lists && tiles > 1 ? read * tiles * 5.0 / 6.6 : side > 1 ? read * 5.0 / 6.2 : read) + 3.3 + 1.4 * (s.batch - 1) / n;
+  cut = std::max(cut, !lists && tiles > 1 ? read * tiles * 5.0 / 6.6 : side > 1 ? read * 5.0 / 6.2 : read) + 3.3;
+  if (s.batch > 1) cut += lists ? 1.4 * (s.batch - 1) / n : 2.5 * std::max(1.0, (s.batch - 1) / n);
   cut += std::min(n + s.batch, 2 * n) * units * std::min<int64_t>(32, cols) * s.d * 8 / (lists ? 2.75e6 : 3.5e6);
   return cut < whole;
+}
+// Where there are many column tiles, as many workgroups as fill the card four times share them out, so that units that get short
+// lists take more of them: 32 heads x 128, 5 to 50 % of 500 to 4000 positions, once / four times, longest first: 8 sequences of 128 queries
+// 53.4 / 42.6 us, of 256 101.7 / 77.3, 4 of 1024 182 / 136.
+static int64_t column_groups(int64_t wgs, int64_t tiles) {
+  return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles, 65535), 8 * kUnits / std::max<int64_t>(1, wgs)));
+}
+// Workgroups that share V's columns where lists are whole (see attend_cache_kernel): as many as leave no unit two of them.
+static int32_t v_split_of(const Shape& s, int64_t wgs) {
+  return s.d == 128 && 4 * wgs <= kUnits ? 4 : 2 * wgs <= kUnits ? 2 : 1;
 }
 static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, int64_t total_k) {
   CachePlan p{};
   total_k = std::min<int64_t>(total_k, int64_t(s.batch) * max_k);
   const int64_t heads = lists ? s.hq : s.hkv, cols = lists ? s.max_q : int64_t(s.max_q) * s.group;
   const int64_t tiles = std::max<int64_t>(1, (cols + 31) / 32), units = heads * tiles, resident = 2 * kUnits;
+  const int32_t v_split = v_split_of(s, heads * s.batch * column_groups(heads * s.batch, tiles));
   p.side = 1;
   if (max_k > 0) {
     auto piece_for = [&](int64_t side) {
@@ -557,7 +589,7 @@ static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, i
     // (the ids of a list's rows lie in LDS: no workgroup takes more than kMaxListRows of them, whole or in pieces)
     bool cut = lists && max_k > kMaxListRows;
     if (!cut && !(lists && piece > kMaxListRows))
-      cut = better_in_pieces(s, lists, heads, cols, tiles, max_k, total_k, piece, p.side);
+      cut = better_in_pieces(s, lists, heads, cols, tiles, max_k, total_k, piece, p.side, v_split);
     if (lists) piece = std::min<int64_t>(piece, kMaxListRows);
     if (cut) {
       p.piece = int32_t(std::min<int64_t>(piece, INT32_MAX));
@@ -565,10 +597,8 @@ static CachePlan plan_attend_cached(const Shape& s, bool lists, int32_t max_k, i
     }
   }
   const int64_t wgs = p.piece ? heads / p.side * p.n_pieces : heads * s.batch;
-  // Where there are many column tiles, as many workgroups as fill the card four times share them out, so that units that get short
-  // lists take more of them: 32 heads x 128, 5 to 50 % of 500 to 4000 positions, once / four times, longest first: 8 sequences of 128 queries
-  // 53.4 / 42.6 us, of 256 101.7 / 77.3, 4 of 1024 182 / 136.
-  p.groups = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles, 65535), 4 * resident / std::max<int64_t>(1, wgs)));
+  p.groups = column_groups(wgs, tiles);
+  p.v_split = p.piece ? 1 : v_split;
   if (!p.piece && s.batch <= kRankBatch) {
     if (wgs * p.groups > resident) p.order = kLongestFirst;
     else if (wgs > kUnits && p.groups == 1) p.order = kFolded;
@@ -606,18 +636,23 @@ hipError_t launch_attend_cached(const Shape& s, const CacheView& c, int32_t max_
   const unsigned heads = lists ? s.hq : p.piece ? s.hkv / p.side : s.hkv;
   const unsigned parts = !p.piece ? s.batch : lists || p.n_pieces < 8 ? p.n_pieces : (p.n_pieces + 7) / 8 * 8;
   auto launch = [&](auto kernel, bool heads_first) {
-    const dim3 grid(heads_first ? heads : parts, heads_first ? parts : heads, unsigned(p.groups));
+    const dim3 grid(heads_first ? heads : parts, heads_first ? parts : heads, unsigned(p.groups * p.v_split));
     kernel<<<grid, kWaves * 64, 0, st>>>(qh, c, cu_q, cu_kv, idx, cu_k, total_k, oh, po, pml, p.piece, p.order, s DLLM_CHECK_PASS);
   };
   auto with_d = [&](auto d) {
     constexpr int D = decltype(d)::value;
     if (p.piece) {
-      if (lists) launch(attend_cache_kernel<D, true, true, 1>, true);
-      else if (p.side == kSide) launch(attend_cache_kernel<D, false, true, kSide>, false);
-      else launch(attend_cache_kernel<D, false, true, 1>, false);
+      if (lists) launch(attend_cache_kernel<D, true, true, 1, 1>, true);
+      else if (p.side == kSide) launch(attend_cache_kernel<D, false, true, kSide, 1>, false);
+      else launch(attend_cache_kernel<D, false, true, 1, 1>, false);
     } else {
-      if (lists) launch(attend_cache_kernel<D, true, false, 1>, true);
-      else launch(attend_cache_kernel<D, false, false, 1>, true);
+      auto whole = [&](auto vs) {
+        if (lists) launch(attend_cache_kernel<D, true, false, 1, decltype(vs)::value>, true);
+        else launch(attend_cache_kernel<D, false, false, 1, decltype(vs)::value>, true);
+      };
+      if (p.v_split == D / 32) whole(std::integral_constant<int, D / 32>{});
+      else if (p.v_split == 2) whole(std::integral_constant<int, 2>{});
+      else whole(std::integral_constant<int, 1>{});
     }
   };
   if (s.d == 128) with_d(std::integral_constant<int, 128>{});

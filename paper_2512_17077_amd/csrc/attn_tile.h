@@ -50,6 +50,8 @@ __device__ __forceinline__ int tile_swz(int row) {
   if constexpr (D == 128) {
     const int r = row & 15;
     return ((r & 3) << 2) | (r >> 2);
+  } else if constexpr (D == 32) {
+    return 0;   // rows of 64 bytes: the four that a transposed read takes fill the banks as they lie
   } else {
     const int x = (row >> 1) & 7;
     return ((x & 1) << 2) | (x >> 1);
