@@ -832,7 +832,9 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
     ck0 = cu_k[b]; ck1 = cu_k[b + 1]; kv0 = cu_kv[b]; kv1 = cu_kv[b + 1]; q0 = cu_q[b]; q1 = cu_q[b + 1];
     asm volatile("" : "+s"(ck0), "+s"(ck1), "+s"(kv0), "+s"(kv1), "+s"(q0), "+s"(q1));
   }
-  const int g = (blockIdx.x + b) % s.hkv;   // (rotation: see score_kernel)
+  // (Rotation: see score_kernel.  Rows of codes come faster without it in one round, 8 sequences of 4000 over 32 heads 31.2 -> 29.7 us, 24
+  // of 8192 over 8 53.0 -> 52.3, but not in several, 64 of 3000 to 4000 over 8 66.8 -> 68.1.)
+  const int g = (ES == 1 && !ranked ? blockIdx.x : blockIdx.x + b) % s.hkv;
   if (ck1 == ck0) return;
   const int L = kv1 - kv0, Lc = L - forced_tail, kb = ck1 - ck0 - forced_tail;
   if (kb < 0 || Lc < kb) return;   // broken precondition (see topk_kernel): write nothing
@@ -1295,6 +1297,8 @@ static bool fused_pays_short(const Shape& s, int es, int32_t pool_w) {
   one += pooled * (1.1 + 0.39 * s.group) + wider * (0.065 + 0.12 * s.group) + 0.07 * std::max(0.0, mb - 10.0);
   double two = (s.d == 128 ? 8.6 : 8.1) + (s.group * s.d > 256 ? 1.6 : 0.0) + 0.17 * std::max(0.0, mb - 10.0);
   two += 0.4 * pooled + 0.06 * wider * ((s.max_kv + kTopkThreads - 1) / kTopkThreads);
+  // (codes: more lists than are ranked at once; 29 sequences of 407 to 776, 32 heads over 8, 19.2 us in two launches, 13.8 in one)
+  if (es == 1) two += 4.5 * std::max(0.0, s.batch * s.hq / double(2 * compute_units()) - 1.0);
   return one < two;
 }
 static bool fused_pays(const Shape& s, int es, int32_t pool_w) {
@@ -1302,7 +1306,14 @@ static bool fused_pays(const Shape& s, int es, int32_t pool_w) {
   if (pairs <= cus && s.max_kv <= kFusedWaves * kFusedTilesShort * 64) return fused_pays_short(s, es, pool_w);
   const int64_t rounds = (pairs + cus - 1) / cus;
   const bool full = rounds == 1 ? 4 * pairs >= 3 * cus : 5 * pairs >= 4 * rounds * cus;
-  const bool even = 4 * int64_t(s.total_kv) >= 3 * int64_t(s.batch) * s.max_kv;
+  bool even = 4 * int64_t(s.total_kv) >= 3 * int64_t(s.batch) * s.max_kv;
+  if (es == 1) {
+    // Codes stream faster, so that the ranking, which one launch does for one list per compute unit at a time, weighs more: several rounds only
+    // for long lists of four heads (27 sequences of 315, 32 heads, window 5, 33.3 us in one launch, 18.4 in two; 28 of 4791, 16 heads x 64,
+    // 60.6 / 57.9), and four heads, scored on the matrix cores, in one round down to half full (32 of 2000 to 8000, 53.5 / 62.1).
+    if (rounds > 1 && (s.group < 4 || s.max_kv <= kFusedWaves * kFusedTilesShort * 64)) return false;
+    if (rounds == 1 && s.group == 4 && pool_w == 1) even = 2 * int64_t(s.total_kv) >= int64_t(s.batch) * s.max_kv;
+  }
   return full && even;
 }
 
