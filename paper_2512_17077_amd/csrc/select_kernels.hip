@@ -141,7 +141,11 @@ __device__ __forceinline__ void for_each_index(F& f, std::integer_sequence<int, 
 }
 
 // Scales: nothing, or KeyScales with ES = 1 (e4m3 codes; the queries are bf16).
-template <int ES, int D, int GT, bool Once, typename... Scales>
+// HW: KV heads per workgroup (codes only).  The rows of two heads lie side by side, at head_dim 64 in one 128-byte line, and come faster if
+// they are asked for together; the sums of both are there at once as long as no thread has more than one of them to make.  Selection in two launches,
+// one head per workgroup / two: 16 heads x 64, twenty sequences of 500 to 4000 20.8 / 16.6 us, 40 heads x 64, nineteen of 4866 96.2 / 77.5;
+// 32 x 128, eight of 4000 31.7 / 31.0; with groups 8 x 128, 24 of 1000 to 8192 44.8 / 48.8.  (Four: 16.3, 78.5, 33.7 and 58.5.)
+template <int ES, int D, int GT, bool Once, int HW, typename... Scales>
 __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void score_kernel(
     const char* __restrict__ k, const char* __restrict__ q, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ cu_kv, const int32_t* __restrict__ cu_k, float* __restrict__ scores,
@@ -155,7 +159,7 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   constexpr bool kMatrix = ES == 1 && GT == 4;
   constexpr int SD = kSumPitch<ES, D, GT>;
   __shared__ v4u tile[kScoreWaves][64 * CH];
-  extern __shared__ __attribute__((aligned(16))) float sums[];   // [group][D]: block sums of this KV head's query heads
+  extern __shared__ __attribute__((aligned(16))) float sums[];   // [HW * group][D]: block sums of the KV heads' query heads
 
   // KV head is the fastest grid index: workgroups launched together read neighbouring 2*D-byte
   // slices of the same token rows, which keeps the DRAM pages they open busy.  Consecutive workgroups
@@ -163,7 +167,10 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   // fetch the same 1/8 of the 256-byte columns (measured: 4 % on the batched workload).  Within a
   // sequence an XCD keeps its heads, so their block queries are fetched into its L2 once (rotating by
   // the row block as well cost 12 % more bytes fetched on the grouped-query workload).
-  const int b = blockIdx.z, g = (blockIdx.x + blockIdx.z) % s.hkv;
+  constexpr int SPW = kScoreWaves / HW;   // waves per head
+  static_assert(HW == 1 || ES == 1, "heads side by side: codes only");
+  const int side = HW == 1 ? 0 : __builtin_amdgcn_readfirstlane(int(threadIdx.x) / (SPW * 64));
+  const int b = blockIdx.z, g0 = HW == 1 ? (blockIdx.x + blockIdx.z) % s.hkv : (blockIdx.x + blockIdx.z) % (s.hkv / HW) * HW, g = g0 + side;
   // All offsets in one round trip: the memory system is busy with the K stream, and every dependent
   // scalar load before the first tile request costs this workgroup a microsecond or more.
   int ck0 = cu_k[b], ck1 = cu_k[b + 1], kv0 = cu_kv[b], kv1 = cu_kv[b + 1], q0 = cu_q[b], q1 = cu_q[b + 1];
@@ -171,8 +178,8 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   if (ck1 == ck0) return;
   const int L = kv1 - kv0;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (blockIdx.y * kScoreWaves * tiles_per_wave * 64 >= L) return;   // the whole workgroup lies past the end
-  const int first = (blockIdx.y * kScoreWaves + wave) * tiles_per_wave * 64;
+  if (blockIdx.y * SPW * tiles_per_wave * 64 >= L) return;   // the whole workgroup lies past the end
+  const int first = (blockIdx.y * SPW + wave - side * SPW) * tiles_per_wave * 64;
   const int ntiles = first < L ? min(tiles_per_wave, (L - first + 63) / 64) : 0;   // 0: only helps with the sums
   const char* base = k + (int64_t(kv0) * s.kv_tok + int64_t(g) * s.kv_head) * ES + (lane % CH) * 16;
   const int64_t row_pitch = s.kv_tok * ES;
@@ -210,8 +217,8 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
       else
         return *reinterpret_cast<const float*>(p);
     };
-    for (int e = threadIdx.x; e < s.group * D; e += kScoreWaves * 64) {
-      const char* p = q + (int64_t(q0) * s.q_tok + int64_t(g * s.group + e / D) * s.q_head + e % D) * QES;
+    for (int e = threadIdx.x; e < HW * s.group * D; e += kScoreWaves * 64) {
+      const char* p = q + (int64_t(q0) * s.q_tok + int64_t(g0 * s.group + e / D) * s.q_head + e % D) * QES;
       float a = 0.0f;
       int i = 0;
       for (; i + 32 <= nq; i += 32) {   // a whole block of 32 queries: all loads in flight, then the adds in row order
@@ -240,7 +247,7 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   constexpr int NQ = D / 16;
   float vq[kMatrix ? 1 : GT][NQ];
   auto load_sums = [&](int hh) {
-    const float* qs = sums + hh * D + (lane & 15);
+    const float* qs = sums + (HW == 1 ? hh : side * s.group + hh) * D + (lane & 15);
     if constexpr (!kMatrix) {
 #pragma unroll
       for (int t = 0; t < GT; ++t)
@@ -1215,11 +1222,13 @@ static hipError_t launch_score(const Shape& s, const void* k, const void* q, con
   static_assert(kScoreRowsPerBlock == 256, "dllm_rule_score_tiles counts in workgroups of four tiles");
   const int tpw = dllm_rule_score_tiles(s.batch, s.total_kv, s.max_kv, s.hkv, s.group, D * ES);
   const int rows_per_block = kScoreRowsPerBlock * tpw;
-  dim3 grid(s.hkv, (s.max_kv + rows_per_block - 1) / rows_per_block, s.batch);
+  const bool pairs = ES == 1 && s.hkv % 2 == 0 && s.group * D <= 128;
+  const int rows = pairs ? rows_per_block / 2 : rows_per_block;
+  dim3 grid(pairs ? s.hkv / 2 : s.hkv, (s.max_kv + rows - 1) / rows, s.batch);
   dim3 block(kScoreWaves * 64);
   const char *kp = static_cast<const char*>(k), *qp = static_cast<const char*>(q);
   // dynamic LDS beside the 64 * 2*D-byte tiles
-  const size_t sums_bytes = size_t(s.group) * (s.group % 4 == 0 ? kSumPitch<ES, D, 4> : D) * sizeof(float);
+  const size_t sums_bytes = size_t(pairs ? 2 : 1) * s.group * (s.group % 4 == 0 ? kSumPitch<ES, D, 4> : D) * sizeof(float);
   auto launch = [&](auto kernel) -> hipError_t {
     const hipError_t ea = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                               hipFuncAttributeMaxDynamicSharedMemorySize, int(sums_bytes));
@@ -1227,14 +1236,21 @@ static hipError_t launch_score(const Shape& s, const void* k, const void* q, con
     kernel<<<grid, block, sums_bytes, st>>>(kp, qp, cu_q, cu_kv, cu_k, scores, tpw, s, scales... DLLM_CHECK_PASS);
     return hipGetLastError();
   };
-  if (streams_once(s, ES)) {
-    if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, true, Scales...>);
-    if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, true, Scales...>);
-    return launch(score_kernel<ES, D, 1, true, Scales...>);
+  const bool once = streams_once(s, ES);
+  if constexpr (ES == 1) {
+    if (pairs && s.group == 1) return once ? launch(score_kernel<ES, D, 1, true, 2, Scales...>) : launch(score_kernel<ES, D, 1, false, 2, Scales...>);
+    if constexpr (D == 64) {
+      if (pairs) return once ? launch(score_kernel<ES, D, 2, true, 2, Scales...>) : launch(score_kernel<ES, D, 2, false, 2, Scales...>);
+    }
   }
-  if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, false, Scales...>);
-  if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, false, Scales...>);
-  return launch(score_kernel<ES, D, 1, false, Scales...>);
+  if (once) {
+    if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, true, 1, Scales...>);
+    if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, true, 1, Scales...>);
+    return launch(score_kernel<ES, D, 1, true, 1, Scales...>);
+  }
+  if (s.group % 4 == 0) return launch(score_kernel<ES, D, 4, false, 1, Scales...>);
+  if (s.group % 2 == 0) return launch(score_kernel<ES, D, 2, false, 1, Scales...>);
+  return launch(score_kernel<ES, D, 1, false, 1, Scales...>);
 }
 
 static std::atomic<int32_t> g_select_form{DLLM_SELECT_FORM_AUTO};

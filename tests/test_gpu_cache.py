@@ -363,6 +363,14 @@ def test_select_the_longest_list_and_many_sequences():
     check_select(c, 16, [2] * 150, [max(1, n // 2) for n in lens], 44, pool_w=3)
 
 
+@pytest.mark.parametrize("hq,hkv,d,lens", [
+    (16, 16, 64, [2000 + 61 * b for b in range(12)]),   # pairs of heads, several tiles per wave
+    (6, 3, 64, [900, 64, 129, 700]),                    # no pairs
+    (2, 2, 128, [127, 128, 129, 1, 3000])])
+def test_select_with_two_heads_per_workgroup_and_without(hq, hkv, d, lens):
+    check_select(filled(lens, hkv, d, 16, 53), hq, [32] * len(lens), [(n + 4) // 5 for n in lens], 54)
+
+
 @pytest.mark.parametrize("hq,hkv,batch,n", [(16, 16, 16, 1024), (32, 8, 24, 2100), (32, 32, 9, 700)])
 def test_select_batches_that_take_one_launch_or_stream_k_once(hq, hkv, batch, n):
     c = filled([n - 13 * b for b in range(batch)], hkv, 128, 32, 51)
