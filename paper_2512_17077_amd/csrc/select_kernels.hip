@@ -824,7 +824,12 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
   // of up to 64 sequences) the slots go down the sequences by length, longest first: workgroups start in
   // the order of their numbers, so the compute units that come free first pick up the longest lists
   // left and the rounds end level whatever the mix of lengths.
-  int b = blockIdx.x / s.hkv;
+  constexpr bool kHalfLines = ES * D == 64;   // rows of 64 bytes: two heads share a 128-byte line
+  uint32_t at = blockIdx.x;
+  if constexpr (kHalfLines) {   // ... so they go to one XCD and its L2 (workgroup i runs on XCD i % 8; 64 sequences of 4000 to 8000, 43.0 -> 33.9 us)
+    if (s.hkv % 2 == 0 && (at | 15u) < gridDim.x) at = 2 * (at / 16 * 8 + at % 8) + at / 8 % 2;
+  }
+  int b = at / s.hkv;
   int ck0, ck1, kv0, kv1, q0, q1;
   if (ranked) {
     const int ln = threadIdx.x & 63, i = min(ln, s.batch - 1);
@@ -841,7 +846,7 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
   }
   // (Rotation: see score_kernel.  Rows of codes come faster without it in one round, 8 sequences of 4000 over 32 heads 31.2 -> 29.7 us, 24
   // of 8192 over 8 53.0 -> 52.3, but not in several, 64 of 3000 to 4000 over 8 66.8 -> 68.1.)
-  const int g = (ES == 1 && !ranked ? blockIdx.x : blockIdx.x + b) % s.hkv;
+  const int g = (ES == 1 && (kHalfLines || !ranked) ? at : at + b) % s.hkv;
   if (ck1 == ck0) return;
   const int L = kv1 - kv0, Lc = L - forced_tail, kb = ck1 - ck0 - forced_tail;
   if (kb < 0 || Lc < kb) return;   // broken precondition (see topk_kernel): write nothing
