@@ -345,7 +345,7 @@ dllm_status dllm_hcsa_select_cached(const dllm_batch *batch, const dllm_cache *c
  */
 size_t dllm_hcsa_attend_cached_workspace(const dllm_batch *batch, const dllm_cache *cache, int32_t max_k);
 /*
- * How a call shares out its work, for tests and measurement: 0 if every list goes to a workgroup of its own, else the rows per piece
+ * How a call shares out its work, for tests and measurement: 0 if every list is taken whole, else the rows per piece
  * in which the lists, laid end to end, are cut (lists that a cut goes through are merged by a second launch); -1 if the arguments
  * are invalid.  lists: 1 for a call with idx, 0 for one without.  Host only: no device memory is read, nothing launched.
  */

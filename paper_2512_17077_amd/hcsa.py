@@ -397,7 +397,19 @@ def _cached_stream(batch: DllmBatch, cache: DllmCache, stream) -> int:
     device = torch.cuda.current_device()
     if device != cache.of[3]:
         raise ValueError(f"the tensors are on device {cache.of[3]}, the current device is {device}")
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError(f"the stream is on device {stream.device_index}, the current device is {device}")
+    return stream.cuda_stream
+
+
+def _workspace_on(nbytes: int, device, stream) -> Optional[torch.Tensor]:
+    """A workspace of the call's own; on another stream than the current one it stays reserved until that stream is done with it."""
+    workspace = _workspace(nbytes, device)
+    if workspace is not None and stream is not None:
+        workspace.record_stream(stream)
+    return workspace
 
 
 def _rows_moved(batch: DllmBatch, cu_rows, total_rows: int, at) -> int:
@@ -442,13 +454,13 @@ def dllm_hcsa_select_cached(batch: DllmBatch, cache: DllmCache, cu_k: torch.Tens
                             idx_out: torch.Tensor, pool_w: int = 1, forced_tail: int = 0, head_sum: bool = False,
                             workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Selection over the cached K (batch: make_cached_batch); fills idx_out [Hq, total_k] (int32, device)."""
-    stream = _cached_stream(batch, cache, stream)
+    raw = _cached_stream(batch, cache, stream)
     if workspace is None:
-        workspace = _workspace(dllm_hcsa_select_cached_workspace(batch, cache, max_k), idx_out.device)
+        workspace = _workspace_on(dllm_hcsa_select_cached_workspace(batch, cache, max_k), idx_out.device, stream)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_select_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_k), int(total_k), int(max_k),
                                          int(pool_w), int(forced_tail), int(bool(head_sum)), _ptr(idx_out), _ptr(workspace),
-                                         nbytes, stream))
+                                         nbytes, raw))
     return idx_out
 
 
@@ -457,7 +469,7 @@ def dllm_hcsa_attend_cached_workspace(batch: DllmBatch, cache: DllmCache, max_k:
 
 
 def dllm_hcsa_attend_cached_form_of(batch: DllmBatch, cache: DllmCache, lists: bool, max_k: int, total_k: int) -> int:
-    """Rows per piece in which a call cuts its lists, 0 if every list goes to a workgroup of its own."""
+    """Rows per piece in which a call cuts its lists, 0 if every list is taken whole."""
     piece = int(lib().dllm_hcsa_attend_cached_form_of(ctypes.byref(batch), ctypes.byref(cache), int(bool(lists)), int(max_k),
                                                       int(total_k)))
     if piece < 0:
@@ -468,10 +480,10 @@ def dllm_hcsa_attend_cached_form_of(batch: DllmBatch, cache: DllmCache, lists: b
 def dllm_hcsa_attend_cached(batch: DllmBatch, cache: DllmCache, idx: Optional[torch.Tensor], cu_k: torch.Tensor, total_k: int,
                             max_k: int, o: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention over the cache: every head over its own list, or (idx None) all heads over the first rows of each sequence."""
-    stream = _cached_stream(batch, cache, stream)
+    raw = _cached_stream(batch, cache, stream)
     if workspace is None:
-        workspace = _workspace(dllm_hcsa_attend_cached_workspace(batch, cache, max_k), o.device)
+        workspace = _workspace_on(dllm_hcsa_attend_cached_workspace(batch, cache, max_k), o.device, stream)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_attend_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(idx), _ptr(cu_k), int(total_k),
-                                         int(max_k), _ptr(o), _ptr(workspace), nbytes, stream))
+                                         int(max_k), _ptr(o), _ptr(workspace), nbytes, raw))
     return o

@@ -200,6 +200,12 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         hcsa.dllm_hcsa_select_cached(b, c, cu, 4, 4, torch.zeros((2, 4), dtype=torch.int32))
     with pytest.raises(ValueError, match="device 1"):
         hcsa.dllm_hcsa_attend_cached(b, c, None, cu, 4, 4, q)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+
+    class OfDevice0:
+        device_index, cuda_stream = 0, 0
+    with pytest.raises(ValueError, match="stream is on device 0"):
+        hcsa.dllm_hcsa_attend_cached(b, c, None, cu, 4, 4, q, stream=OfDevice0())
 
 
 def shaped(rng):

@@ -644,6 +644,31 @@ def test_calls_are_the_same_every_time_and_on_another_stream():
         assert torch.equal(one.view(torch.int16), two.view(torch.int16))
 
 
+def test_a_call_on_a_busy_stream_keeps_its_workspace():
+    """A call that makes its own workspace, on a stream with work ahead of it: memory that the current stream takes next is other memory."""
+    lens, hq = [9000, 4000], 4
+    c = filled(lens, 2, 64, 32, 175)
+    q = normal(64, hq, 64, torch.bfloat16, 176)
+    cu_q, cu_k = (torch.tensor(cu32(x), device=DEV) for x in ([32, 32], lens))
+    batch = hcsa.make_cached_batch(q, cu_q, c.cu_t, c.total, 2, 32, 9000, 0.125)
+    want, got, busy = torch.empty_like(q), torch.empty_like(q), torch.ones((4096, 4096), device=DEV)
+    idx = [torch.full((hq, 13000), -1, dtype=torch.int32, device=DEV) for _ in range(2)]
+    hcsa.dllm_hcsa_attend_cached(batch, c.desc, None, cu_k, 13000, 9000, want)
+    hcsa.dllm_hcsa_select_cached(batch, c.desc, cu_k, 13000, 9000, idx[0])
+    assert hcsa.dllm_hcsa_attend_cached_form_of(batch, c.desc, False, 9000, 13000) > 0   # (parts go through the workspace)
+    sizes = [f(batch, c.desc, 9000) for f in (hcsa.dllm_hcsa_attend_cached_workspace, hcsa.dllm_hcsa_select_cached_workspace)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(8):
+            torch.mm(busy, busy)
+    hcsa.dllm_hcsa_attend_cached(batch, c.desc, None, cu_k, 13000, 9000, got, stream=side)
+    hcsa.dllm_hcsa_select_cached(batch, c.desc, cu_k, 13000, 9000, idx[1], stream=side)
+    taken = [torch.full((n,), 255, dtype=torch.uint8, device=DEV) for n in sizes]
+    torch.cuda.synchronize()
+    assert torch.equal(want.view(torch.int16), got.view(torch.int16)) and torch.equal(*idx) and all(bool((t == 255).all()) for t in taken)
+
+
 @pytest.mark.parametrize("decode", [False, True])
 def test_a_step_replayed_from_a_hip_graph(decode):
     """Two graphs that share their workspaces, replayed in turn with new rows, queries and places, beside eager work; every
