@@ -525,6 +525,16 @@ def test_attention_of_many_queries(hq, hkv, d, qlens, lens, lists):
     check_attend(filled(lens, hkv, d, 16, 87), hq, qlens, [n - n // 3 for n in lens], 88, lists)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(64, 1, 128), (33, 1, 64), (68, 2, 64)])
+def test_many_query_heads_on_one_kv_head(hq, hkv, d):
+    """More query heads per KV head than a column tile has places, single tokens and blocks."""
+    c = filled([700, 33, 1, 2049], hkv, d, 16, 191)
+    check_select(c, hq, [32, 1, 3, 8], [200, 5, 1, 700], 192)
+    for qlens in ([1, 1, 1, 1], [9, 1, 4, 2]):
+        for lists in (True, False):
+            check_attend(c, hq, qlens, [650, 33, 1, 1500], 193, lists)
+
+
 @pytest.mark.parametrize("lists", [True, False])
 def test_large_scores_and_strided_queries(lists):
     c = filled([400, 333], 2, 128, 32, 91, layout="padded")
