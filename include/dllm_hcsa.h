@@ -271,12 +271,11 @@ dllm_status dllm_dense_refresh_attend(const dllm_batch *batch,
  *
  * A write chooses the smallest scale that the block's largest magnitude over 448 allows, between 2^-95 and 2^119, and rounds
  * value / scale to the nearest code, ties to even: finite values of magnitude up to 448 * 2^119 are off by at most 2^-4 of
- * themselves or 2^-10 of the scale, whichever is more; larger ones are stored as 448 * 2^119, infinities and NaN as NaN (they
- * do not count for the scale).
- * Memory of a new cache must be zero where a part of a block may be written before the rest of it.
- * Limits (DLLM_ERR_UNSUPPORTED beyond them): total_kv <= 2^31 - 129; a write or read moves fewer than 2^24 (block, four heads of K or V) pairs of
- * one sequence; attention takes sequences of up to 2^24 tokens that span less than 4 GiB of codes, with stride_tok < 2^24, and
- * lists of up to 2^27 - 2048 rows per head together.
+ * themselves or 2^-10 of the scale, whichever is more; larger ones are stored as 448 * 2^119, infinities and NaN as NaN (they do
+ * not count for the scale).  Memory of a new cache must be zero where a part of a block may be written before the rest of it.
+ * Limits (DLLM_ERR_UNSUPPORTED beyond them): total_kv <= 2^31 - 129; a write or read moves fewer than 2^24 (block, four heads of
+ * K or V) pairs of one sequence; attention takes sequences of up to 2^24 tokens that span less than 4 GiB of codes, with
+ * stride_tok < 2^24, and lists of up to 2^27 - 2048 rows per head together.
  */
 typedef struct {
   uint8_t *k, *v;                  /* device, 16-byte aligned; codes of [total_kv, n_kv_heads, head_dim] */
@@ -292,14 +291,14 @@ int64_t dllm_hcsa_cache_scale_slots(int32_t total_kv, int32_t batch, int32_t sca
  * Write rows into the cache, quantising them.
  *
  * batch describes the cache's sequences (batch, n_kv_heads, head_dim, cu_kv, total_kv, max_kv) and the rows to be written: k and
- * v with kv_stride_*, of type dtype (bf16 or fp32), [total_rows, n_kv_heads, head_dim].  Its q, cu_q, total_q, max_q, q_stride_* and
- * softmax_scale are not read.  Rows cu_rows[b] .. cu_rows[b+1]-1 go to positions at[b] .. of sequence b; with at == NULL to its last positions;
- * with cu_rows == NULL every sequence is written whole (total_rows must be total_kv; max_rows and at are not read).  max_rows
- * bounds the rows of a sequence.  Rows that would lie outside their sequence are left out.
- * A block of which rows stay as they were (rows of the sequence that this call does not write) keeps at least its scale; where the
- * new rows need a larger one, the rows that stay move to it (exactly, but for values below 2^-6 of the new scale, which are
- * rounded again).  Writing the same rows again changes nothing.
- * Needs no workspace.  Calls that write into one block at the same time (different streams) race.
+ * v with kv_stride_*, of type dtype (bf16 or fp32), [total_rows, n_kv_heads, head_dim].  Its q, cu_q, total_q, max_q, q_stride_*
+ * and softmax_scale are not read.  Rows cu_rows[b] .. cu_rows[b+1]-1 go to positions at[b] .. of sequence b; with at == NULL to
+ * its last positions; with cu_rows == NULL every sequence is written whole (total_rows must be total_kv; max_rows and at are not
+ * read).  max_rows bounds the rows of a sequence.  Rows that would lie outside their sequence are left out.  A block of which rows
+ * stay as they were (rows of the sequence that this call does not write) keeps at least its scale; where the new rows need a
+ * larger one, the rows that stay move to it (exactly, but for values below 2^-6 of the new scale, which are rounded again).
+ * Writing the same rows again changes nothing.  Needs no workspace.  Calls that write into one block at the same time (different
+ * streams) race.
  */
 dllm_status dllm_hcsa_cache_write(const dllm_batch *batch, const dllm_cache *cache,
                                   const int32_t *cu_rows, /* device, [batch+1], or NULL */
@@ -307,8 +306,9 @@ dllm_status dllm_hcsa_cache_write(const dllm_batch *batch, const dllm_cache *cac
                                   const int32_t *at,      /* device, [batch], or NULL */
                                   void *hip_stream);
 /*
- * Read rows back: the same ranges in the other direction, values code * scale in dtype (exact in bf16 and in fp32).  k_out and v_out take the
- * place of batch->k and batch->v (not read) and have their strides.  Rows outside their sequence are left as they were.
+ * Read rows back: the same ranges in the other direction, values code * scale in dtype (exact in bf16 and in fp32).  k_out and
+ * v_out take the place of batch->k and batch->v (not read) and have their strides.  Rows outside their sequence are left as they
+ * were.
  */
 dllm_status dllm_hcsa_cache_read(const dllm_batch *batch, const dllm_cache *cache,
                                  const int32_t *cu_rows, /* device, [batch+1], or NULL */
@@ -334,14 +334,14 @@ dllm_status dllm_hcsa_select_cached(const dllm_batch *batch, const dllm_cache *c
 
 /*
  * Attention over the cache: dllm_hcsa_attend without densely attended sequences, K and V from the cache.  dtype is that of q and
- * o and must be DLLM_BF16; k, v and kv_stride_* of batch are not read.  With idx every head attends over its own list; with idx ==
- * NULL all heads of a sequence attend over its rows 0 .. k_b-1, which are then read once per KV head: for single tokens of an
- * autoregressive model (cu_kv gives every sequence's room, cu_k how much of it is filled) or a block over everything.  A
- * sequence with k_b == 0 gets zeros.  A query whose scores are NaN, overflow to plus infinity or are all minus infinity, or that attends
- * over a NaN, gets NaN; no other query's output changes.  A row that no query attends over may hold anything.
- * The rows are read once per 32 queries (without lists: per 32 query-head pairs of a group), so for blocks of 128
- * queries and more over everything dllm_hcsa_cache_read and dllm_dense_refresh_attend together take less time.
- * The workspace query serves calls with and without idx; unless max_k or max_q is 0 it is never 0.
+ * o and must be DLLM_BF16; k, v and kv_stride_* of batch are not read.  With idx every head attends over its own list; with idx
+ * == NULL all heads of a sequence attend over its rows 0 .. k_b-1, which are then read once per KV head: for single tokens of an
+ * autoregressive model (cu_kv gives every sequence's room, cu_k how much of it is filled) or a block over everything.  A sequence
+ * with k_b == 0 gets zeros.  A query whose scores are NaN, overflow to plus infinity or are all minus infinity, or that attends
+ * over a NaN, gets NaN; no other query's output changes.  A row that no query attends over may hold anything. The rows are read
+ * once per 32 queries (without lists: per 32 query-head pairs of a group), so for blocks of 128 queries and more over everything
+ * dllm_hcsa_cache_read and dllm_dense_refresh_attend together take less time. The workspace query serves calls with and without
+ * idx; unless max_k or max_q is 0 it is never 0.
  */
 size_t dllm_hcsa_attend_cached_workspace(const dllm_batch *batch, const dllm_cache *cache, int32_t max_k);
 /*

@@ -561,8 +561,8 @@ int32_t dllm_hcsa_attend_cached_form_of(const dllm_batch* batch, const dllm_cach
   dllm::CacheView view;
   if (check_cached_call(batch, cache, &s, &view) != DLLM_OK) return -1;
   if ((lists != 0 && lists != 1) || total_k < 0 || max_k < 0 || max_k > total_k || max_k > batch->max_kv) {
-    fail(DLLM_ERR_INVALID_ARG, "need lists 0 or 1 and 0 <= max_k <= min(total_k, max_kv) (got %d, max_k=%d, total_k=%d, max_kv=%d)", lists,
-         max_k, total_k, batch->max_kv);
+    fail(DLLM_ERR_INVALID_ARG, "need lists 0 or 1 and 0 <= max_k <= min(total_k, max_kv) (got %d, max_k=%d, total_k=%d, max_kv=%d)",
+         lists, max_k, total_k, batch->max_kv);
     return -1;
   }
   return dllm::attend_cached_piece(s, lists != 0, max_k, total_k);
@@ -585,7 +585,8 @@ dllm_status dllm_hcsa_attend_cached(const dllm_batch* batch, const dllm_cache* c
                 "one sequence must have at most 2^24 rows spanning < 4 GiB with a token stride < 16 MiB (max_kv=%d, stride_tok=%lld)",
                 batch->max_kv, static_cast<long long>(view.tok));
   if (idx != nullptr && total_k > (1 << 27) - 2048)   // (pieces of 2048 rows at most, and no more of them than a grid's y takes)
-    return fail(DLLM_ERR_UNSUPPORTED, "lists of more than 2^27 - 2048 rows per head together are not taken in one call (total_k=%d)", total_k);
+    return fail(DLLM_ERR_UNSUPPORTED, "lists of more than 2^27 - 2048 rows per head together are not taken in one call (total_k=%d)",
+                total_k);
   if ((st = check_workspace(workspace, workspace_bytes, dllm::attend_cached_workspace(s, max_k))) != DLLM_OK) return st;
   g_err[0] = 0;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);

@@ -5,18 +5,19 @@
 //            model, or a block over everything).  The query heads of a group then read the same rows, so a tile's 32
 //            columns are (query, head of the group) pairs of one KV head and the rows are read once per group.
 //
-// With scores z_ij = scale * q_i . k_j (in units of log 2) an output is sum_j 2^(z_ij - m_i) v_j / sum_j 2^(z_ij - m_i), in one pass
-// over the rows with the running maximum m_i and sum; parts of a list that different waves or workgroups have seen are joined by
-// weighting them with 2^(m_part - m).  A code times its scale is a bf16 value exactly, so the arithmetic is that of a bf16 cache:
-// probabilities are rounded to bf16 for the matrix cores (the sum adds the rounded ones, so that weights still sum to one), outputs once at the end.
+// With scores z_ij = scale * q_i . k_j (in units of log 2) an output is sum_j 2^(z_ij - m_i) v_j / sum_j 2^(z_ij - m_i), in one
+// pass over the rows with the running maximum m_i and sum; parts of a list that different waves or workgroups have seen are
+// joined by weighting them with 2^(m_part - m).  A code times its scale is a bf16 value exactly, so the arithmetic is that of a
+// bf16 cache: probabilities are rounded to bf16 for the matrix cores (the sum adds the rounded ones, so that weights still sum to
+// one), outputs once at the end.
 //
 // What bounds it: the rows, each read once (a block of 32 queries does 64 operations per byte of them, the matrix cores
 // could do 350 meanwhile).  Gathered rows of 128 bytes come at 4.0 TB/s at best, rows in order at 6.7; a
 // workgroup alone gets through a row of K and V in 7 ns, which decides where there are few lists.  So:
-//   - A workgroup of four waves walks one list or piece of one (or of four heads, see kSide).  Each wave has a span of 32-row tiles of its own and LDS that
-//     no other wave touches, so the walk needs no workgroup barrier.
-//   - A tile's rows are fetched one tile ahead at head_dim 128, two at 64, into registers.  (Two ahead at 128: 24.6 us against 23.4 on sixteen
-//     ragged lists, 32 heads; the registers are better spent on operands.)
+//   - A workgroup of four waves walks one list or piece of one (or of four heads, see kSide).  Each wave has a span of 32-row
+//     tiles of its own and LDS that no other wave touches, so the walk needs no workgroup barrier.
+//   - A tile's rows are fetched one tile ahead at head_dim 128, two at 64, into registers.  (Two ahead at 128: 24.6 us against
+//     23.4 on sixteen ragged lists, 32 heads; the registers are better spent on operands.)
 //   - K goes into LDS as codes and is converted on its way into the matrix cores (half the LDS traffic of converting before);
 //     there a lane's 16 bytes are 16 elements of one row, and the queries, which stay in registers, are fetched in that
 //     order.  V, which is read transposed, 16 bits at a time, is converted first.  The conversion applies the scale.
@@ -79,23 +80,25 @@ __device__ __forceinline__ int sequence_at(const int32_t* __restrict__ cu_k, int
   return lo;
 }
 
-// Order in which lists that are taken whole are started.  Two workgroups are resident per compute unit, and workgroup i shares its
-// unit with workgroup i + 256 (measured: see below), so where all lists are resident but not one per unit, the longest are
+// Order in which lists that are taken whole are started.  Two workgroups are resident per compute unit, and workgroup i shares
+// its unit with workgroup i + 256 (measured: see below), so where all lists are resident but not one per unit, the longest are
 // left alone and the others folded, shortest with longest: with pairs = lists beyond 256, the first `pairs` places go to the
-// shortest, in rising order, the next to the longest, and those that come second are in falling order.  32 heads x 128, lists of 5 to 50 % of 512 to
-// 4096 positions, mean over six draws, as they come / longest first / folded: 9 sequences 18.2 / 19.5 / 17.4 us, 12 24.6 / 23.6 / 20.4, 14
-// 27.8 / 26.1 / 22.1, 16 28.9 / 27.7 / 25.2.  With more lists than are resident, longest first: 20 sequences 35.8 / 32.3.
+// shortest, in rising order, the next to the longest, and those that come second are in falling order.  32 heads x 128, lists of
+// 5 to 50 % of 512 to 4096 positions, mean over six draws, as they come / longest first / folded: 9 sequences 18.2 / 19.5 / 17.4
+// us, 12 24.6 / 23.6 / 20.4, 14 27.8 / 26.1 / 22.1, 16 28.9 / 27.7 / 25.2.  With more lists than are resident, longest first: 20
+// sequences 35.8 / 32.3.
 enum : int { kAsTheyCome = 0, kLongestFirst = 1, kFolded = 2 };
 constexpr int kUnits = 256;   // compute units
 
-// Heads side by side (HW): in pieces without lists a workgroup's four waves can take a piece of four neighbouring KV heads, each wave one
-// of them and all of the piece, instead of a quarter of the piece of one head.  The rows of four heads lie side by side in memory, and
-// asked for together they come faster (reading alone, 8 heads x 128 codes: 6.7 TB/s against 5.6 to 6.0), and no merge of the
-// waves is left.  But a wave then has four times as many tiles one after the other.  8 heads x 128, single tokens, a head per workgroup /
-// four: 32 sequences of 4000 to 8192 72.8 / 67.2 us, 12 36.6 / 33.0, one of 8000 (pieces of 128, the least) 10.9 / 11.9; 4 heads, 8 of
-// 3000 to 8000 (160) 17.9 / 16.4; 16 heads x 64, 40 of 1000 to 5000 (896) 63.3 / 56.1, 4 x 64, 30 of 1000 to 8000 (288) 22.1 / 22.6.  So
-// from pieces of 160 rows on at head_dim 128, 512 at 64, and up to four column tiles (which read the rows again, from the caches: 24 sequences of 500
-// to 4000, 16 queries of 32 heads over 8, 53.4 / 49.7; 4 of 512 queries, 32 heads, 204 / 216).
+// Heads side by side (HW): in pieces without lists a workgroup's four waves can take a piece of four neighbouring KV heads, each
+// wave one of them and all of the piece, instead of a quarter of the piece of one head.  The rows of four heads lie side by side
+// in memory, and asked for together they come faster (reading alone, 8 heads x 128 codes: 6.7 TB/s against 5.6 to 6.0), and no
+// merge of the waves is left.  But a wave then has four times as many tiles one after the other.  8 heads x 128, single tokens, a
+// head per workgroup / four: 32 sequences of 4000 to 8192 72.8 / 67.2 us, 12 36.6 / 33.0, one of 8000 (pieces of 128, the least)
+// 10.9 / 11.9; 4 heads, 8 of 3000 to 8000 (160) 17.9 / 16.4; 16 heads x 64, 40 of 1000 to 5000 (896) 63.3 / 56.1, 4 x 64, 30 of
+// 1000 to 8000 (288) 22.1 / 22.6.  So from pieces of 160 rows on at head_dim 128, 512 at 64, and up to four column tiles (which
+// read the rows again, from the caches: 24 sequences of 500 to 4000, 16 queries of 32 heads over 8, 53.4 / 49.7; 4 of 512
+// queries, 32 heads, 204 / 216).
 constexpr int kSide = 4;
 
 // Rows are shared out in pieces (Pieces): the lists of one head, laid end to end as cu_k has them, are cut every `piece` rows, and
@@ -132,9 +135,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
   constexpr bool kHeadsFirst = Lists || !Pieces;
   int unit = kHeadsFirst ? blockIdx.x : blockIdx.y, px = kHeadsFirst ? blockIdx.y : blockIdx.x;
   if constexpr (kHeadsFirst && (D == 64 || Lists)) {
-    // Heads that share memory go to one XCD and its L2 (workgroup i runs on XCD i % 8): the lists of the query heads of one KV head, and the two
-    // heads whose 64-byte rows share a 128-byte line.  Of 8 * share workgroups in a row, every eighth belongs to one set.  Lists of
-    // 5 to 50 % of 512 to 4096, sixteen sequences, 32 heads over 8 x 128 25.4 -> 24.0 us, 40 sequences of 30 to 50 % 69.2 -> 60.7.
+    // Heads that share memory go to one XCD and its L2 (workgroup i runs on XCD i % 8): the lists of the query heads of one KV
+    // head, and the two heads whose 64-byte rows share a 128-byte line.  Of 8 * share workgroups in a row, every eighth belongs
+    // to one set.  Lists of 5 to 50 % of 512 to 4096, sixteen sequences, 32 heads over 8 x 128 25.4 -> 24.0 us, 40 sequences of
+    // 30 to 50 % 69.2 -> 60.7.
     const uint32_t n = gridDim.x, at = blockIdx.x + n * blockIdx.y;
     const uint32_t share = (Lists ? s.group : 1) * (D == 64 && s.hkv % 2 == 0 ? 2 : 1);
     if (share > 1 && (at / (8 * share) + 1) * (8 * share) <= n * gridDim.y) {
@@ -147,10 +151,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
   const int h0 = Lists ? unit : g * s.group;                      // its first query head
   const int heads = Lists ? 1 : s.group;
   const int span = wave % SP;
-  // VS: workgroups that share a list's columns of V, where there are units to spare.  One unit gets 36 GB/s of gathered rows, with eight
-  // waves no more than with four, so that each takes all of K and its part of V, and needs no merge: lists of 256 / 512 / 1024 rows,
-  // 32 heads x 128, alone 7.14 / 9.45 / 14.1 us, in four 5.72 / 7.22 / 10.7; four of 276 to 994 in two 13.0 -> 11.3; single tokens of two
-  // sequences of 847 and 738, 8 KV heads, in four 12.1 -> 8.7.  (Two workgroups per unit: 11.3 -> 17.3.)
+  // VS: workgroups that share a list's columns of V, where there are units to spare.  One unit gets 36 GB/s of gathered rows,
+  // with eight waves no more than with four, so that each takes all of K and its part of V, and needs no merge: lists of 256 /
+  // 512 / 1024 rows, 32 heads x 128, alone 7.14 / 9.45 / 14.1 us, in four 5.72 / 7.22 / 10.7; four of 276 to 994 in two 13.0 ->
+  // 11.3; single tokens of two sequences of 847 and 738, 8 KV heads, in four 12.1 -> 8.7.  (Two workgroups per unit: 11.3 ->
+  // 17.3.)
   const int part = VS > 1 ? int(blockIdx.z) % VS : 0;   // of V's columns
   const int qt0 = VS > 1 ? int(blockIdx.z) / VS : blockIdx.z, qt_step = gridDim.z / VS;   // column tiles
   // column x of a sequence: query x / heads, head h0 + x % heads
@@ -534,17 +539,18 @@ static int64_t pieces_per_head(const Shape& s, int64_t units) {
   return std::max<int64_t>(1, (s.d == 128 ? kUnits : 2 * kUnits) / units);
 }
 // Lists whole or in pieces: the less of two sums, in us, from these measurements.
-//   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6, whole lists in order 6.0; with half of V 0.78 of that, with a
-//   quarter 0.72), two on one unit 0.7 of their sum; where there are more than two, every one takes 4.5 us beside its rows.
-//   The card reads gathered rows at 4.9 TB/s, rows in order at 5.0, at 6.2 with heads side by side, at 4.2 where every list is a
-//   workgroup's own (3.5 where two share V's columns; 64-byte rows two thirds of all that; it includes starting and draining).
-//   Without lists every column tile reads the rows again, from the caches, in pieces at 6.6 TB/s.
-//   Pieces cost a second launch and its latencies (3.3), what is written and read again (2.75 TB/s, without lists 3.5), and for the further
-//   sequences that a piece reaches into 1.4 each with lists, in the mean, 2.5 without, in the piece that has most.
-// One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 15.5 / 9.4; 32 of 4000 to 8192 79.2 / 67.2;
-// 16 of 1000 12.2 / 17.4; 40 of 100 to 1000 16.1 / 19.4; lists of 32 heads x 128, one of 4096 rows 25.9 / 14.5, of 1024 10.7 / 10.0, of 256 5.7 / 9.5; four
-// of 276 to 994 11.3 / 16.9; sixteen of 5 to 50 % of 512 to 4096 23.3 / 36.3.  Over 700 batches, 1 to 40 sequences of 128 to 8192, the
-// choice is 0.3 % above the better one in the mean, 43 % at most (single tokens of 25 sequences of 3440, 4 heads x 64, 25.7 against 18.0).
+//   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6, whole lists in order 6.0; with half of V 0.78 of that,
+//   with a quarter 0.72), two on one unit 0.7 of their sum; where there are more than two, every one takes 4.5 us beside its
+//   rows. The card reads gathered rows at 4.9 TB/s, rows in order at 5.0, at 6.2 with heads side by side, at 4.2 where every list
+//   is a workgroup's own (3.5 where two share V's columns; 64-byte rows two thirds of all that; it includes starting and
+//   draining). Without lists every column tile reads the rows again, from the caches, in pieces at 6.6 TB/s. Pieces cost a second
+//   launch and its latencies (3.3), what is written and read again (2.75 TB/s, without lists 3.5), and for the further sequences
+//   that a piece reaches into 1.4 each with lists, in the mean, 2.5 without, in the piece that has most.
+// One sequence of 8000 rows, single tokens, 32 heads over 8 x 128: whole 66.7, in pieces 10.4; of 2000 rows 15.5 / 9.4; 32 of
+// 4000 to 8192 79.2 / 67.2; 16 of 1000 12.2 / 17.4; 40 of 100 to 1000 16.1 / 19.4; lists of 32 heads x 128, one of 4096 rows 25.9
+// / 14.5, of 1024 10.7 / 10.0, of 256 5.7 / 9.5; four of 276 to 994 11.3 / 16.9; sixteen of 5 to 50 % of 512 to 4096 23.3 / 36.3.
+// Over 700 batches, 1 to 40 sequences of 128 to 8192, the choice is 0.3 % above the better one in the mean, 43 % at most (single
+// tokens of 25 sequences of 3440, 4 heads x 64, 25.7 against 18.0).
 static bool better_in_pieces(const Shape& s, bool lists, int64_t heads, int64_t cols, int64_t tiles, int64_t max_k, int64_t total_k,
                              int64_t piece, int64_t side, int32_t v_split) {
   const double row_us = s.d == 128 ? 7.0e-3 : 4.6e-3, units = double(heads * tiles), n = double((total_k + piece - 1) / piece);
@@ -562,8 +568,8 @@ static bool better_in_pieces(const Shape& s, bool lists, int64_t heads, int64_t 
   return cut < whole;
 }
 // Where there are many column tiles, as many workgroups as fill the card four times share them out, so that units that get short
-// lists take more of them: 32 heads x 128, 5 to 50 % of 500 to 4000 positions, once / four times, longest first: 8 sequences of 128 queries
-// 53.4 / 42.6 us, of 256 101.7 / 77.3, 4 of 1024 182 / 136.
+// lists take more of them: 32 heads x 128, 5 to 50 % of 500 to 4000 positions, once / four times, longest first: 8 sequences of
+// 128 queries 53.4 / 42.6 us, of 256 101.7 / 77.3, 4 of 1024 182 / 136.
 static int64_t column_groups(int64_t wgs, int64_t tiles) {
   return std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(tiles, 65535), 8 * kUnits / std::max<int64_t>(1, wgs)));
 }

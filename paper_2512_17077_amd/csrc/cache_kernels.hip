@@ -9,11 +9,11 @@
 // bf16 or fp32 without a rounding), and rows that stay in a block whose scale grows move to the new one without a second
 // rounding (but where they fall below 2^-6 * u).
 //
-// Both kernels only move data: bytes in and out decide.  One wave takes one block of one head of K or of V, so that the
-// maximum needs no workgroup barrier and all rows of the block are in flight at once; the four waves of a workgroup take
-// neighbouring heads, whose rows are neighbours in memory.  Measured (MI355X, 32 heads x 128, a plain copy 5.2 TB/s): 16 sequences of 512
-// to 4096 rows written from bf16, 847 MB in and out, 146 us, 5.8 TB/s; 8 of 2048 read back, 403 MB, 70 us, 5.7 TB/s; a block of 32 rows 5.5
-// us, the time of a launch.
+// Both kernels only move data: bytes in and out decide.  One wave takes one block of one head of K or of V, so that the maximum
+// needs no workgroup barrier and all rows of the block are in flight at once; the four waves of a workgroup take neighbouring
+// heads, whose rows are neighbours in memory.  Measured (MI355X, 32 heads x 128, a plain copy 5.2 TB/s): 16 sequences of 512 to
+// 4096 rows written from bf16, 847 MB in and out, 146 us, 5.8 TB/s; 8 of 2048 read back, 403 MB, 70 us, 5.7 TB/s; a block of 32
+// rows 5.5 us, the time of a launch.
 #include <type_traits>
 
 #include "common.h"

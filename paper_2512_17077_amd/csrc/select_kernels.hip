@@ -140,11 +140,11 @@ __device__ __forceinline__ void for_each_index(F& f, std::integer_sequence<int, 
   (f(std::integral_constant<int, C>{}), ...);
 }
 
-// Scales: nothing, or KeyScales with ES = 1 (e4m3 codes; the queries are bf16).
-// HW: KV heads per workgroup (codes only).  The rows of two heads lie side by side, at head_dim 64 in one 128-byte line, and come faster if
-// they are asked for together; the sums of both are there at once as long as no thread has more than one of them to make.  Selection in two launches,
-// one head per workgroup / two: 16 heads x 64, twenty sequences of 500 to 4000 20.8 / 16.6 us, 40 heads x 64, nineteen of 4866 96.2 / 77.5;
-// 32 x 128, eight of 4000 31.7 / 31.0; with groups 8 x 128, 24 of 1000 to 8192 44.8 / 48.8.  (Four: 16.3, 78.5, 33.7 and 58.5.)
+// Scales: nothing, or KeyScales with ES = 1 (e4m3 codes; the queries are bf16). HW: KV heads per workgroup (codes only).  The
+// rows of two heads lie side by side, at head_dim 64 in one 128-byte line, and come faster if they are asked for together; the
+// sums of both are there at once as long as no thread has more than one of them to make.  Selection in two launches, one head per
+// workgroup / two: 16 heads x 64, twenty sequences of 500 to 4000 20.8 / 16.6 us, 40 heads x 64, nineteen of 4866 96.2 / 77.5; 32
+// x 128, eight of 4000 31.7 / 31.0; with groups 8 x 128, 24 of 1000 to 8192 44.8 / 48.8.  (Four: 16.3, 78.5, 33.7 and 58.5.)
 template <int ES, int D, int GT, bool Once, int HW, typename... Scales>
 __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void score_kernel(
     const char* __restrict__ k, const char* __restrict__ q, const int32_t* __restrict__ cu_q,
@@ -170,7 +170,8 @@ __global__ __launch_bounds__(kScoreWaves * 64, (ES * D <= 256 ? 2 : 1)) void sco
   constexpr int SPW = kScoreWaves / HW;   // waves per head
   static_assert(HW == 1 || ES == 1, "heads side by side: codes only");
   const int side = HW == 1 ? 0 : __builtin_amdgcn_readfirstlane(int(threadIdx.x) / (SPW * 64));
-  const int b = blockIdx.z, g0 = HW == 1 ? (blockIdx.x + blockIdx.z) % s.hkv : (blockIdx.x + blockIdx.z) % (s.hkv / HW) * HW, g = g0 + side;
+  const int b = blockIdx.z;
+  const int g0 = HW == 1 ? (blockIdx.x + blockIdx.z) % s.hkv : (blockIdx.x + blockIdx.z) % (s.hkv / HW) * HW, g = g0 + side;
   // All offsets in one round trip: the memory system is busy with the K stream, and every dependent
   // scalar load before the first tile request costs this workgroup a microsecond or more.
   int ck0 = cu_k[b], ck1 = cu_k[b + 1], kv0 = cu_kv[b], kv1 = cu_kv[b + 1], q0 = cu_q[b], q1 = cu_q[b + 1];
@@ -826,7 +827,8 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
   // left and the rounds end level whatever the mix of lengths.
   constexpr bool kHalfLines = ES * D == 64;   // rows of 64 bytes: two heads share a 128-byte line
   uint32_t at = blockIdx.x;
-  if constexpr (kHalfLines) {   // ... so they go to one XCD and its L2 (workgroup i runs on XCD i % 8; 64 sequences of 4000 to 8000, 43.0 -> 33.9 us)
+  if constexpr (kHalfLines) {
+    // ... so they go to one XCD and its L2 (workgroup i runs on XCD i % 8; 64 sequences of 4000 to 8000, 43.0 -> 33.9 us)
     if (s.hkv % 2 == 0 && (at | 15u) < gridDim.x) at = 2 * (at / 16 * 8 + at % 8) + at / 8 % 2;
   }
   int b = at / s.hkv;
@@ -844,8 +846,8 @@ __global__ __launch_bounds__(kFusedWaves * 64) __attribute__((amdgpu_waves_per_e
     ck0 = cu_k[b]; ck1 = cu_k[b + 1]; kv0 = cu_kv[b]; kv1 = cu_kv[b + 1]; q0 = cu_q[b]; q1 = cu_q[b + 1];
     asm volatile("" : "+s"(ck0), "+s"(ck1), "+s"(kv0), "+s"(kv1), "+s"(q0), "+s"(q1));
   }
-  // (Rotation: see score_kernel.  Rows of codes come faster without it in one round, 8 sequences of 4000 over 32 heads 31.2 -> 29.7 us, 24
-  // of 8192 over 8 53.0 -> 52.3, but not in several, 64 of 3000 to 4000 over 8 66.8 -> 68.1.)
+  // (Rotation: see score_kernel.  Rows of codes come faster without it in one round, 8 sequences of 4000 over 32 heads 31.2 ->
+  // 29.7 us, 24 of 8192 over 8 53.0 -> 52.3, but not in several, 64 of 3000 to 4000 over 8 66.8 -> 68.1.)
   const int g = (ES == 1 && (kHalfLines || !ranked) ? at : at + b) % s.hkv;
   if (ck1 == ck0) return;
   const int L = kv1 - kv0, Lc = L - forced_tail, kb = ck1 - ck0 - forced_tail;
@@ -1243,7 +1245,8 @@ static hipError_t launch_score(const Shape& s, const void* k, const void* q, con
   };
   const bool once = streams_once(s, ES);
   if constexpr (ES == 1) {
-    if (pairs && s.group == 1) return once ? launch(score_kernel<ES, D, 1, true, 2, Scales...>) : launch(score_kernel<ES, D, 1, false, 2, Scales...>);
+    if (pairs && s.group == 1)
+      return once ? launch(score_kernel<ES, D, 1, true, 2, Scales...>) : launch(score_kernel<ES, D, 1, false, 2, Scales...>);
     if constexpr (D == 64) {
       if (pairs) return once ? launch(score_kernel<ES, D, 2, true, 2, Scales...>) : launch(score_kernel<ES, D, 2, false, 2, Scales...>);
     }
@@ -1329,9 +1332,10 @@ static bool fused_pays(const Shape& s, int es, int32_t pool_w) {
   const bool full = rounds == 1 ? 4 * pairs >= 3 * cus : 5 * pairs >= 4 * rounds * cus;
   bool even = 4 * int64_t(s.total_kv) >= 3 * int64_t(s.batch) * s.max_kv;
   if (es == 1) {
-    // Codes stream faster, so that the ranking, which one launch does for one list per compute unit at a time, weighs more: several rounds only
-    // for long lists of four heads (27 sequences of 315, 32 heads, window 5, 33.3 us in one launch, 18.4 in two; 28 of 4791, 16 heads x 64,
-    // 60.6 / 57.9), and four heads, scored on the matrix cores, in one round down to half full (32 of 2000 to 8000, 53.5 / 62.1).
+    // Codes stream faster, so that the ranking, which one launch does for one list per compute unit at a time, weighs more:
+    // several rounds only for long lists of four heads (27 sequences of 315, 32 heads, window 5, 33.3 us in one launch, 18.4 in
+    // two; 28 of 4791, 16 heads x 64, 60.6 / 57.9), and four heads, scored on the matrix cores, in one round down to half full
+    // (32 of 2000 to 8000, 53.5 / 62.1).
     if (rounds > 1 && (s.group < 4 || s.max_kv <= kFusedWaves * kFusedTilesShort * 64)) return false;
     if (rounds == 1 && s.group == 4 && pool_w == 1) even = 2 * int64_t(s.total_kv) >= int64_t(s.batch) * s.max_kv;
   }
