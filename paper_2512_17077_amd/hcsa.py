@@ -208,10 +208,17 @@ def make_batch(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Te
     return b
 
 
-def _workspace(nbytes: int, device) -> Optional[torch.Tensor]:
+def _workspace(nbytes: int, device, stream=None) -> Optional[torch.Tensor]:
+    """A workspace of the call's own.  It is allocated on the stream that works in it: memory of another stream's pool may
+    still be read or written by what is queued there, for which this stream would not wait."""
     if nbytes == 0:
         return None
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)   # torch allocations are >= 256-byte aligned
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)   # torch allocations are >= 256-byte aligned
+    if not isinstance(stream, torch.cuda.Stream):   # (anything with a raw stream will do)
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def dllm_hcsa_select_workspace(batch: DllmBatch, max_k: int) -> int:
@@ -222,7 +229,7 @@ def dllm_hcsa_select(batch: DllmBatch, cu_k: torch.Tensor, total_k: int, max_k: 
                      pool_w: int = 1, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Per-head top-k selection; fills idx_out [Hq, total_k] (int32, device)."""
     if workspace is None:
-        workspace = _workspace(dllm_hcsa_select_workspace(batch, max_k), idx_out.device)
+        workspace = _workspace(dllm_hcsa_select_workspace(batch, max_k), idx_out.device, stream)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_select(ctypes.byref(batch), _ptr(cu_k), int(total_k), int(max_k), int(pool_w),
                                   _ptr(idx_out), _ptr(workspace), nbytes, _stream(stream)))
@@ -234,7 +241,7 @@ def dllm_hcsa_select_ex(batch: DllmBatch, cu_k: torch.Tensor, total_k: int, max_
                         workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Selection with the block's own positions always kept and / or one list shared by all heads."""
     if workspace is None:
-        workspace = _workspace(dllm_hcsa_select_workspace(batch, max_k), idx_out.device)
+        workspace = _workspace(dllm_hcsa_select_workspace(batch, max_k), idx_out.device, stream)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_select_ex(ctypes.byref(batch), _ptr(cu_k), int(total_k), int(max_k), int(pool_w),
                                      int(forced_tail), int(bool(head_sum)), _ptr(idx_out), _ptr(workspace), nbytes,
@@ -285,7 +292,7 @@ def dllm_hcsa_attend(batch: DllmBatch, idx: Optional[torch.Tensor], cu_k: Option
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention over kept rows (and over all rows for sequences flagged dense); fills o."""
     if workspace is None:
-        workspace = _workspace(dllm_hcsa_attend_workspace(batch, max_k), o.device)
+        workspace = _workspace(dllm_hcsa_attend_workspace(batch, max_k), o.device, stream)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_attend(ctypes.byref(batch), _ptr(idx), _ptr(cu_k), int(total_k), int(max_k),
                                   _ptr(seq_mode), _ptr(o), _ptr(workspace), nbytes, _stream(stream)))
@@ -404,14 +411,6 @@ def _cached_stream(batch: DllmBatch, cache: DllmCache, stream) -> int:
     return stream.cuda_stream
 
 
-def _workspace_on(nbytes: int, device, stream) -> Optional[torch.Tensor]:
-    """A workspace of the call's own; on another stream than the current one it stays reserved until that stream is done with it."""
-    workspace = _workspace(nbytes, device)
-    if workspace is not None and stream is not None:
-        workspace.record_stream(stream)
-    return workspace
-
-
 def _rows_moved(batch: DllmBatch, cu_rows, total_rows: int, at) -> int:
     """Rows of batch's tensors that a write or read moves, checked."""
     if cu_rows is None:
@@ -456,7 +455,7 @@ def dllm_hcsa_select_cached(batch: DllmBatch, cache: DllmCache, cu_k: torch.Tens
     """Selection over the cached K (batch: make_cached_batch); fills idx_out [Hq, total_k] (int32, device)."""
     raw = _cached_stream(batch, cache, stream)
     if workspace is None:
-        workspace = _workspace_on(dllm_hcsa_select_cached_workspace(batch, cache, max_k), idx_out.device, stream)
+        workspace = _workspace(dllm_hcsa_select_cached_workspace(batch, cache, max_k), idx_out.device, stream)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_select_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_k), int(total_k), int(max_k),
                                          int(pool_w), int(forced_tail), int(bool(head_sum)), _ptr(idx_out), _ptr(workspace),
@@ -482,7 +481,7 @@ def dllm_hcsa_attend_cached(batch: DllmBatch, cache: DllmCache, idx: Optional[to
     """Attention over the cache: every head over its own list, or (idx None) all heads over the first rows of each sequence."""
     raw = _cached_stream(batch, cache, stream)
     if workspace is None:
-        workspace = _workspace_on(dllm_hcsa_attend_cached_workspace(batch, cache, max_k), o.device, stream)
+        workspace = _workspace(dllm_hcsa_attend_cached_workspace(batch, cache, max_k), o.device, stream)
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _raise(lib().dllm_hcsa_attend_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(idx), _ptr(cu_k), int(total_k),
                                          int(max_k), _ptr(o), _ptr(workspace), nbytes, raw))

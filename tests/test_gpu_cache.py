@@ -679,6 +679,48 @@ def test_a_call_on_a_busy_stream_keeps_its_workspace():
     assert torch.equal(want.view(torch.int16), got.view(torch.int16)) and torch.equal(*idx) and all(bool((t == 255).all()) for t in taken)
 
 
+def test_a_call_on_an_idle_stream_takes_no_memory_that_the_current_stream_still_reads():
+    """Tensors as large as the workspaces, freed while a copy of them waits behind other work; then calls on a stream that does not wait."""
+    lens, hq = [9000, 4000], 4
+    c = filled(lens, 2, 64, 32, 177)
+    q = normal(64, hq, 64, torch.bfloat16, 178)
+    cu_q, cu_k = (torch.tensor(cu32(x), device=DEV) for x in ([32, 32], lens))
+    cached = hcsa.make_cached_batch(q, cu_q, c.cu_t, c.total, 2, 32, 9000, 0.125)
+    k, v = read_back(c)
+    dense = hcsa.make_batch(q, k, v, cu_q, c.cu_t, 32, 9000, 0.125)
+
+    def calls(stream):
+        o, idx = ([torch.full(shape, -1, dtype=t, device=DEV) for _ in range(2)] for shape, t in ((q.shape, q.dtype), ((hq, 13000), torch.int32)))
+        torch.cuda.synchronize()
+        yield o + idx
+        hcsa.dllm_hcsa_attend_cached(cached, c.desc, None, cu_k, 13000, 9000, o[0], stream=stream)
+        hcsa.dllm_hcsa_select_cached(cached, c.desc, cu_k, 13000, 9000, idx[0], stream=stream)
+        hcsa.dllm_hcsa_select_ex(dense, cu_k, 13000, 9000, idx[1], stream=stream)
+        hcsa.dllm_hcsa_attend(dense, idx[1], cu_k, 13000, 9000, None, o[1], stream=stream)
+        yield
+
+    first = calls(None)
+    want = next(first)
+    next(first)
+    side, busy = torch.cuda.Stream(), torch.ones((4096, 4096), device=DEV)
+    sizes = [f(b, c.desc, 9000) for f, b in ((hcsa.dllm_hcsa_attend_cached_workspace, cached), (hcsa.dllm_hcsa_select_cached_workspace, cached))]
+    sizes += [f(dense, 9000) for f in (hcsa.dllm_hcsa_select_workspace, hcsa.dllm_hcsa_attend_workspace)]
+    assert min(sizes) > 0
+    held = [torch.full((n,), 7, dtype=torch.uint8, device=DEV) for n in sizes]
+    seen = [torch.zeros_like(t) for t in held]
+    second = calls(side)
+    got = next(second)
+    for _ in range(8):
+        torch.mm(busy, busy)
+    for t, x in zip(seen, held):
+        t.copy_(x)
+    del held, t, x
+    next(second)
+    torch.cuda.synchronize()
+    assert all(bool((t == 7).all()) for t in seen)
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and int(got[2].min()) >= 0
+
+
 @pytest.mark.parametrize("decode", [False, True])
 def test_a_step_replayed_from_a_hip_graph(decode):
     """Two graphs that share their workspaces, replayed in turn with new rows, queries and places, beside eager work; every
