@@ -328,6 +328,12 @@ def make_packed_batch(q: torch.Tensor, k_packed: torch.Tensor, v_packed: torch.T
 
 
 # ---------------------------------------------------------------- the 8-bit cache
+# (Checks of a call cost the host 0.1 us an attribute, where the smallest calls take 5 us in all.)
+def _fits(t: torch.Tensor, dtype: torch.dtype, shape, place: int) -> bool:
+    """What the kernels take a tensor for: its type, this shape without gaps, on the device numbered `place`."""
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == place
+
+
 def cache_scale_slots(total_kv: int, batch: int, scale_block: int) -> int:
     """Entries of one head's row of scales in a cache of `batch` sequences with total_kv tokens together."""
     n = int(lib().dllm_hcsa_cache_scale_slots(int(total_kv), int(batch), int(scale_block)))
@@ -354,6 +360,7 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale:
     # (not part of the C structure: the tensors stay alive with their descriptor, and what the checks of a call compare)
     c.tensors = (k, v, k_scale, v_scale)
     c.of = (int(k.shape[0]), int(k.shape[1]), int(k.shape[2]), k.device.index)
+    c.place = k.get_device()
     c.most_sequences = int(k_scale.shape[1]) - int(k.shape[0]) // c.scale_block
     return c
 
@@ -361,11 +368,12 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale:
 def make_cached_batch(q: torch.Tensor, cu_q: torch.Tensor, cu_kv: torch.Tensor, total_kv: int, n_kv_heads: int, max_q: int,
                       max_kv: int, softmax_scale: float) -> DllmBatch:
     """Describe packed queries q [total_q,Hq,D] and the sequences of a cache (select_cached, attend_cached)."""
-    assert q.dim() == 3 and q.stride(2) == 1 and cu_q.dtype == torch.int32 and cu_kv.dtype == torch.int32
+    assert q.dim() == 3 and q.stride(2) == 1
     b = DllmBatch()
     b.dtype = {torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16}[q.dtype]
     b.batch = cu_q.numel() - 1
-    assert cu_kv.numel() == b.batch + 1
+    for cu in (cu_q, cu_kv):
+        assert _fits(cu, torch.int32, (b.batch + 1,), q.get_device()), "cu_q and cu_kv: contiguous int32 [batch + 1], on q's device"
     b.n_q_heads, b.n_kv_heads, b.head_dim = q.shape[1], int(n_kv_heads), q.shape[2]
     b.q = q.data_ptr()
     b.q_stride_tok, b.q_stride_head = q.stride(0), q.stride(1)
@@ -375,16 +383,18 @@ def make_cached_batch(q: torch.Tensor, cu_q: torch.Tensor, cu_kv: torch.Tensor, 
     b.softmax_scale = float(softmax_scale)
     b.tensors = (q, cu_q, cu_kv)   # (as in make_cache)
     b.of, b.sequences = (b.total_kv, b.n_kv_heads, b.head_dim, q.device.index), b.batch
+    b.q_shape, b.q_dtype, b.cu_shape = q.shape, q.dtype, cu_q.shape
     return b
 
 
 def make_rows_batch(k: torch.Tensor, v: torch.Tensor, cu_kv: torch.Tensor, total_kv: int, max_kv: int) -> DllmBatch:
     """Describe rows k/v [total_rows,Hkv,D] (bf16 or fp32) and the sequences of the cache that they go to or come from."""
     assert k.dim() == 3 and k.stride(2) == 1 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
-    assert cu_kv.dtype == torch.int32
     b = DllmBatch()
     b.dtype = {torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16}[k.dtype]
     b.batch = cu_kv.numel() - 1
+    assert _fits(cu_kv, torch.int32, (b.batch + 1,), k.get_device()), "cu_kv: contiguous int32 [batch + 1], on the rows' device"
+    assert v.get_device() == k.get_device(), "k and v are on different devices"
     b.n_q_heads = b.n_kv_heads = k.shape[1]
     b.head_dim = k.shape[2]
     b.k, b.v = k.data_ptr(), v.data_ptr()
@@ -393,7 +403,7 @@ def make_rows_batch(k: torch.Tensor, v: torch.Tensor, cu_kv: torch.Tensor, total
     b.total_kv, b.max_kv = int(total_kv), int(max_kv)
     b.tensors = (k, v, cu_kv)   # (as in make_cache)
     b.of, b.sequences = (b.total_kv, b.n_kv_heads, b.head_dim, k.device.index), b.batch
-    b.rows = int(k.shape[0])
+    b.rows, b.place = int(k.shape[0]), k.get_device()
     return b
 
 
@@ -416,8 +426,9 @@ def _rows_moved(batch: DllmBatch, cu_rows, total_rows: int, at) -> int:
     if cu_rows is None:
         assert at is None and batch.rows >= batch.of[0], "without cu_rows all rows are moved"
         return batch.of[0]
-    assert cu_rows.dtype is torch.int32 and cu_rows.numel() == batch.sequences + 1
-    assert at is None or (at.dtype is torch.int32 and at.numel() == batch.sequences and at.is_contiguous())
+    place = batch.place
+    assert _fits(cu_rows, torch.int32, (batch.sequences + 1,), place), "cu_rows: contiguous int32 [batch + 1], on the rows' device"
+    assert at is None or _fits(at, torch.int32, (batch.sequences,), place), "at: contiguous int32 [batch], on the rows' device"
     assert batch.rows >= total_rows, "fewer rows than total_rows"
     return total_rows
 
@@ -428,8 +439,9 @@ def dllm_hcsa_cache_write(batch: DllmBatch, cache: DllmCache, cu_rows: Optional[
     sequence b (at None: its last ones), or every sequence whole (cu_rows None)."""
     total_rows = _rows_moved(batch, cu_rows, total_rows, at)
     stream = _cached_stream(batch, cache, stream)
-    _raise(lib().dllm_hcsa_cache_write(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, max_rows, _ptr(at),
-                                       stream))
+    status = (_lib or lib()).dllm_hcsa_cache_write(batch, cache, _ptr(cu_rows), total_rows, max_rows, _ptr(at), stream)
+    if status:
+        _raise(status)
     return cache
 
 
@@ -440,8 +452,7 @@ def dllm_hcsa_cache_read(batch: DllmBatch, cache: DllmCache, k_out: torch.Tensor
     assert (batch.k or 0) == k_out.data_ptr() and (batch.v or 0) == v_out.data_ptr(), "batch describes other tensors"
     total_rows = _rows_moved(batch, cu_rows, total_rows, at)
     stream = _cached_stream(batch, cache, stream)
-    _raise(lib().dllm_hcsa_cache_read(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_rows), total_rows, max_rows, _ptr(at),
-                                      batch.k, batch.v, stream))
+    _raise(lib().dllm_hcsa_cache_read(batch, cache, _ptr(cu_rows), total_rows, max_rows, _ptr(at), batch.k, batch.v, stream))
     return k_out, v_out
 
 
@@ -453,13 +464,19 @@ def dllm_hcsa_select_cached(batch: DllmBatch, cache: DllmCache, cu_k: torch.Tens
                             idx_out: torch.Tensor, pool_w: int = 1, forced_tail: int = 0, head_sum: bool = False,
                             workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Selection over the cached K (batch: make_cached_batch); fills idx_out [Hq, total_k] (int32, device)."""
-    raw = _cached_stream(batch, cache, stream)
+    raw, place = _cached_stream(batch, cache, stream), cache.place
+    assert _fits(cu_k, torch.int32, batch.cu_shape, place), "cu_k: contiguous int32 [batch + 1], on the cache's device"
+    assert _fits(idx_out, torch.int32, (batch.n_q_heads, total_k), place), "idx_out: contiguous int32 [Hq, total_k], on the cache's device"
     if workspace is None:
         workspace = _workspace(dllm_hcsa_select_cached_workspace(batch, cache, max_k), idx_out.device, stream)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _raise(lib().dllm_hcsa_select_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(cu_k), int(total_k), int(max_k),
-                                         int(pool_w), int(forced_tail), int(bool(head_sum)), _ptr(idx_out), _ptr(workspace),
-                                         nbytes, raw))
+    space, nbytes = None, 0
+    if workspace is not None:
+        assert workspace.is_contiguous() and workspace.get_device() == place, "the workspace is not contiguous or on another device"
+        space, nbytes = workspace.data_ptr(), workspace.nbytes
+    status = (_lib or lib()).dllm_hcsa_select_cached(batch, cache, cu_k.data_ptr(), int(total_k), int(max_k), int(pool_w),
+                                                     int(forced_tail), int(bool(head_sum)), idx_out.data_ptr(), space, nbytes, raw)
+    if status:
+        _raise(status)
     return idx_out
 
 
@@ -479,10 +496,19 @@ def dllm_hcsa_attend_cached_form_of(batch: DllmBatch, cache: DllmCache, lists: b
 def dllm_hcsa_attend_cached(batch: DllmBatch, cache: DllmCache, idx: Optional[torch.Tensor], cu_k: torch.Tensor, total_k: int,
                             max_k: int, o: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention over the cache: every head over its own list, or (idx None) all heads over the first rows of each sequence."""
-    raw = _cached_stream(batch, cache, stream)
+    raw, place = _cached_stream(batch, cache, stream), cache.place
+    assert _fits(cu_k, torch.int32, batch.cu_shape, place), "cu_k: contiguous int32 [batch + 1], on the cache's device"
+    assert idx is None or _fits(idx, torch.int32, (batch.n_q_heads, total_k), place), \
+        "idx: contiguous int32 [Hq, total_k], on the cache's device"
+    assert _fits(o, batch.q_dtype, batch.q_shape, place), "o: contiguous, of q's type and shape, on the cache's device"
     if workspace is None:
         workspace = _workspace(dllm_hcsa_attend_cached_workspace(batch, cache, max_k), o.device, stream)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _raise(lib().dllm_hcsa_attend_cached(ctypes.byref(batch), ctypes.byref(cache), _ptr(idx), _ptr(cu_k), int(total_k),
-                                         int(max_k), _ptr(o), _ptr(workspace), nbytes, raw))
+    space, nbytes = None, 0
+    if workspace is not None:
+        assert workspace.is_contiguous() and workspace.get_device() == place, "the workspace is not contiguous or on another device"
+        space, nbytes = workspace.data_ptr(), workspace.nbytes
+    status = (_lib or lib()).dllm_hcsa_attend_cached(batch, cache, _ptr(idx), cu_k.data_ptr(), int(total_k), int(max_k), o.data_ptr(),
+                                                     space, nbytes, raw)
+    if status:
+        _raise(status)
     return o
