@@ -421,23 +421,25 @@ def _cached_stream(batch: DllmBatch, cache: DllmCache, stream) -> int:
     return stream.cuda_stream
 
 
-def _rows_moved(batch: DllmBatch, cu_rows, total_rows: int, at) -> int:
-    """Rows of batch's tensors that a write or read moves, checked."""
+def _rows_moved(batch: DllmBatch, cu_rows, total_rows: Optional[int], max_rows: Optional[int], at):
+    """(total_rows, max_rows) of a write or read, checked."""
     if cu_rows is None:
         assert at is None and batch.rows >= batch.of[0], "without cu_rows all rows are moved"
-        return batch.of[0]
+        return batch.of[0], 0
+    assert total_rows is not None and max_rows is not None, "cu_rows lies on the device: total_rows and max_rows say what is in it"
     place = batch.place
     assert _fits(cu_rows, torch.int32, (batch.sequences + 1,), place), "cu_rows: contiguous int32 [batch + 1], on the rows' device"
     assert at is None or _fits(at, torch.int32, (batch.sequences,), place), "at: contiguous int32 [batch], on the rows' device"
     assert batch.rows >= total_rows, "fewer rows than total_rows"
-    return total_rows
+    return total_rows, max_rows
 
 
-def dllm_hcsa_cache_write(batch: DllmBatch, cache: DllmCache, cu_rows: Optional[torch.Tensor] = None, total_rows: int = 0,
-                          max_rows: int = 0, at: Optional[torch.Tensor] = None, stream=None) -> DllmCache:
+def dllm_hcsa_cache_write(batch: DllmBatch, cache: DllmCache, cu_rows: Optional[torch.Tensor] = None,
+                          total_rows: Optional[int] = None, max_rows: Optional[int] = None, at: Optional[torch.Tensor] = None,
+                          stream=None) -> DllmCache:
     """Quantise the rows of `batch` (make_rows_batch) into the cache: cu_rows[b] .. cu_rows[b+1]-1 to positions at[b] .. of
     sequence b (at None: its last ones), or every sequence whole (cu_rows None)."""
-    total_rows = _rows_moved(batch, cu_rows, total_rows, at)
+    total_rows, max_rows = _rows_moved(batch, cu_rows, total_rows, max_rows, at)
     stream = _cached_stream(batch, cache, stream)
     status = (_lib or lib()).dllm_hcsa_cache_write(batch, cache, _ptr(cu_rows), total_rows, max_rows, _ptr(at), stream)
     if status:
@@ -446,11 +448,11 @@ def dllm_hcsa_cache_write(batch: DllmBatch, cache: DllmCache, cu_rows: Optional[
 
 
 def dllm_hcsa_cache_read(batch: DllmBatch, cache: DllmCache, k_out: torch.Tensor, v_out: torch.Tensor,
-                         cu_rows: Optional[torch.Tensor] = None, total_rows: int = 0, max_rows: int = 0,
-                         at: Optional[torch.Tensor] = None, stream=None):
+                         cu_rows: Optional[torch.Tensor] = None, total_rows: Optional[int] = None,
+                         max_rows: Optional[int] = None, at: Optional[torch.Tensor] = None, stream=None):
     """Read rows of the cache back into k_out / v_out, the tensors that `batch` describes (make_rows_batch)."""
     assert (batch.k or 0) == k_out.data_ptr() and (batch.v or 0) == v_out.data_ptr(), "batch describes other tensors"
-    total_rows = _rows_moved(batch, cu_rows, total_rows, at)
+    total_rows, max_rows = _rows_moved(batch, cu_rows, total_rows, max_rows, at)
     stream = _cached_stream(batch, cache, stream)
     _raise(lib().dllm_hcsa_cache_read(batch, cache, _ptr(cu_rows), total_rows, max_rows, _ptr(at), batch.k, batch.v, stream))
     return k_out, v_out

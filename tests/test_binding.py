@@ -158,3 +158,18 @@ def test_writes_reads_and_descriptors_refuse_them_too(library):
     hcsa.dllm_hcsa_cache_write(batch, x["cache"], cu, 100, 60, at)
     hcsa.dllm_hcsa_cache_read(batch, x["cache"], *batch.tensors[:2], cu, 100, 60)
     assert len(library.calls) == 2
+
+
+def test_ranges_without_their_sizes_are_refused(library):
+    """(Nothing would be moved, and nothing would say so.)"""
+    x, rows = operands([40, 60]), torch.zeros((100, 2, 64), dtype=torch.bfloat16)
+    batch = hcsa.make_rows_batch(rows, rows.clone(), CU, 100, 60)
+    for sizes in ({}, dict(total_rows=100), dict(max_rows=60)):
+        with pytest.raises(AssertionError):
+            hcsa.dllm_hcsa_cache_write(batch, x["cache"], CU, at=ints(0, 0), **sizes)
+        with pytest.raises(AssertionError):
+            hcsa.dllm_hcsa_cache_read(batch, x["cache"], *batch.tensors[:2], CU, **sizes)
+    assert not library.calls
+    hcsa.dllm_hcsa_cache_write(batch, x["cache"], CU, 0, 0)
+    hcsa.dllm_hcsa_cache_write(batch, x["cache"])
+    assert [call[1][3:5] for call in library.calls] == [(0, 0), (100, 0)]
