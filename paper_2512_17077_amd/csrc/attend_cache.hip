@@ -161,9 +161,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_cache_kernel(
   // column x of a sequence: query x / heads, head h0 + x % heads
   auto query_of = [&](int x) { return Lists ? x : int(uint32_t(x) / uint32_t(heads)); };
   auto clear = [&](int q0, int nq) {   // nothing kept: defined as zeros
-    for (int e = span * 64 + lane; e < nq * heads * D; e += SP * 64) {
-      const int x = e / D, i = query_of(x);
-      o[(int64_t(q0 + i) * s.hq + h0 + (x - i * heads)) * D + e % D] = 0;
+    constexpr int RL = D / 2;   // lanes per row of the output, two elements each (a sequence may have 2^31 elements and more)
+    for (int x = span * (64 / RL) + lane / RL; x < nq * heads; x += SP * (64 / RL)) {
+      const int i = query_of(x);
+      *reinterpret_cast<uint32_t*>(o + (int64_t(q0 + i) * s.hq + h0 + (x - i * heads)) * D + lane % RL * 2) = 0;
     }
   };
 

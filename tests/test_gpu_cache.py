@@ -607,6 +607,19 @@ def test_offsets_beyond_32_bits():
     check_attend(c, 4, [1, 2], [2990, 3100], 125, lists=False)
 
 
+def test_a_sequence_without_kept_rows_and_with_two_thousand_million_outputs():
+    """2^19 queries of 32 heads x 128 over one KV head: zeros, all of them, and so is the sequence behind it."""
+    n, hq, d = 1 << 19, 32, 128
+    c = filled([40, 7], 1, d, 32, 127)
+    q = normal(n + 40, 1, d, torch.bfloat16, 128).as_strided((n + 5, hq, d), (d, d, 1))   # (rows of queries overlap: they are read only)
+    cu_q, cu_k = torch.tensor([0, n, n + 5], dtype=torch.int32, device=DEV), torch.tensor([0, 0, 0], dtype=torch.int32, device=DEV)
+    batch = hcsa.make_cached_batch(q, cu_q, c.cu_t, c.total, 1, n, 40, 0.1)
+    o = torch.full((n + 6, hq, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    hcsa.dllm_hcsa_attend_cached(batch, c.desc, None, cu_k, 0, 0, o[:-1])
+    torch.cuda.synchronize()
+    assert int(torch.count_nonzero(o[:-1].view(torch.int32))) == 0 and bool((o[-1] == 7).all())
+
+
 # ---------------------------------------------------------------- together
 def test_a_denoising_step_on_the_cache():
     """The block's rows go to the end of every sequence, the kept positions always hold them, the block attends."""
