@@ -498,6 +498,24 @@ def test_attention_in_every_form(hq, hkv, d, batch, lo, hi, nq, pieces, lists):
     check_attend(c, hq, [nq] * batch, keep, 86, lists)
 
 
+@pytest.mark.parametrize("hq,hkv,d,batch,lo,hi,nq,pieces", [
+    (16, 16, 64, 19, 50, 400, 2, False), (12, 12, 128, 23, 50, 300, 1, False), (6, 3, 64, 64, 5, 120, 3, False), (9, 3, 64, 90, 5, 120, 3, False),
+    (1, 1, 64, 70, 300, 2500, 1, True), (2, 1, 64, 70, 300, 2500, 33, True), (4, 2, 128, 33, 1, 3000, 2, True), (2, 1, 128, 3, 2000, 9000, 17, True)])
+def test_lists_of_their_own_per_head_in_every_form(hq, hkv, d, batch, lo, hi, nq, pieces):
+    """As above, with every head keeping two thirds of the positions, others than the next head: lists of another head or sequence, or
+    positions taken for rows of the list, would show."""
+    rng = np.random.default_rng(batch)
+    keep = [0 if b in (0, 3, batch - 1) else n for b, n in enumerate(ragged(rng, batch, lo, hi))]
+    lens = [n + n // 2 + 1 for n in keep]
+    c = filled(lens, hkv, d, 32, 85)
+    b = hcsa.make_cached_batch(torch.zeros((nq * batch, hq, d), dtype=torch.bfloat16, device=DEV),
+                               torch.arange(0, nq * batch + 1, nq, dtype=torch.int32, device=DEV), c.cu_t, c.total, hkv, nq, max(lens), 1)
+    assert (hcsa.dllm_hcsa_attend_cached_form_of(b, c.desc, True, max(keep), sum(keep)) > 0) == pieces
+    idx = check_attend(c, hq, [nq] * batch, keep, 86)
+    assert hq == 1 or not np.array_equal(idx[0], idx[1])
+    assert not np.array_equal(idx[0][:keep[1]], np.arange(keep[1]))
+
+
 @pytest.mark.parametrize("hq,hkv,d,nq,lens", [
     (8, 8, 128, 1, [9001, 1, 0, 7003, 4000, 33]),       # single tokens; sequences that a piece holds whole
     (8, 4, 128, 60, [5003, 2, 3000, 0, 1700]),          # several column tiles
@@ -651,6 +669,30 @@ def test_decoding_token_by_token():
         if step % 4 == 3:
             c.check()
             check_attend(c, hq, [1, 1, 1], have, 200 + step, lists=False)
+
+
+@pytest.mark.parametrize("dtype,d,block", [(torch.bfloat16, 64, 16), (torch.float32, 128, 64)])
+def test_memory_of_an_old_cache_serves_a_new_one_once_its_scales_are_zero(dtype, d, block):
+    """Codes of the old rows stay: to the new sequences they are zeros, and no old scale is left to keep."""
+    hkv, room, counts = 2, [150, 90], [37, 64]
+    old = filled([240], hkv, d, block, 155)
+    new = Cache(room, hkv, d, block)
+    for x in "kv":
+        new.t[x].copy_((1000 * old.t[x].view(torch.float8_e4m3fn).float()).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8))
+    assert int((new.t["k"] & 127).min()) < int((new.t["k"] & 127).max()) == 126
+    k, v = (normal(sum(counts), hkv, d, dtype, 157 + i) * 1e-3 for i in range(2))
+    new.write(k, v, [5, 0], counts)
+    new.write(k[:2], 0 * v[:2], [60, 88], [1, 1])   # (zeros alone as well)
+    plus = {x: new.t[x] & torch.where(new.t[x] & 127 > 0, 255, 127).to(torch.uint8) for x in "kv"}   # (-0 as 0)
+    for b, (n, (lo, hi)) in enumerate(zip(room, ((5, 42), (0, 64)))):
+        blocks = {p // block for p in (*range(lo, hi), (60, 88)[b])}
+        for x in "kv":
+            for p in range(n):
+                at, sl = int(new.cu[b]) + p, new.slot(b, p)
+                assert np.array_equal(new.s[x][:, sl].cpu().numpy(), new.want_s[x][:, sl])
+                if p // block in blocks and new.want_s[x][:, sl].all():
+                    want = torch.from_numpy(new.want[x][at] & np.where(new.want[x][at] & 127, 255, 127).astype(np.uint8))
+                    assert torch.equal(plus[x][at].cpu(), want), (x, b, p)
 
 
 def test_calls_are_the_same_every_time_and_on_another_stream():
