@@ -272,7 +272,11 @@ dllm_status dllm_dense_refresh_attend(const dllm_batch *batch,
  * A write chooses the smallest scale that the block's largest magnitude over 448 allows, between 2^-95 and 2^119, and rounds
  * value / scale to the nearest code, ties to even: finite values of magnitude up to 448 * 2^119 are off by at most 2^-4 of
  * themselves or 2^-10 of the scale, whichever is more; larger ones are stored as 448 * 2^119, infinities and NaN as NaN (they do
- * not count for the scale).  Memory of a new cache must be zero where a part of a block may be written before the rest of it.
+ * not count for the scale).  Memory of a new cache must be zero where a part of a block may be written before the rest of it; where
+ * it held another cache before, zero scale bytes are enough (to a write, rows beside scale byte 0 are zeros, whatever finite codes
+ * are left of them).  A part of a block never lowers its scale, so one that was written large once stays so until the block is written
+ * whole.  A scale larger than a block needs costs an element nothing down to 2^-6 of it, and at most 2^-10 of it below; rows that
+ * stay through any number of growing scales are off by less than 2^-4 of themselves plus 2^-9 of the last scale.
  * Limits (DLLM_ERR_UNSUPPORTED beyond them): total_kv <= 2^31 - 129; a write or read moves fewer than 2^24 (block, four heads of
  * K or V) pairs of one sequence; attention takes sequences of up to 2^24 tokens that span less than 4 GiB of codes, with
  * stride_tok < 2^24, and lists of up to 2^27 - 2048 rows per head together.

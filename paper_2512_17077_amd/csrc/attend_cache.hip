@@ -9,11 +9,15 @@
 // pass over the rows with the running maximum m_i and sum; parts of a list that different waves or workgroups have seen are
 // joined by weighting them with 2^(m_part - m).  A code times its scale is a bf16 value exactly, so the arithmetic is that of a
 // bf16 cache: probabilities are rounded to bf16 for the matrix cores (the sum adds the rounded ones, so that weights still sum to
-// one), outputs once at the end.
+// one), outputs once at the end.  Against 64 bits the outputs are off by 1.7e-3 (relative, over all outputs; 256 to 8000 rows), with
+// probabilities in fp32 by 1.6e-3 to 1.7e-3: that is the rounding of the outputs.  The two differ from each other by 6e-4 to 1e-3.
 //
 // What bounds it: the rows, each read once (a block of 32 queries does 64 operations per byte of them, the matrix cores
-// could do 350 meanwhile).  Gathered rows of 128 bytes come at 4.0 TB/s at best, rows in order at 6.7; a
-// workgroup alone gets through a row of K and V in 7 ns, which decides where there are few lists.  So:
+// could do 350 meanwhile).  Gathered rows of 128 bytes, counted once per list and with the call's start and end in the time, come at
+// 3.6 to 4.0 TB/s where lists are taken whole (28 % of sixteen sequences of 512 to 4096 positions, 32 heads: 79 MB in 22.1 us; 30 to
+// 50 % of forty: 288 MB in 72.5), at 4.5 in pieces (half of sixteen of 8192: 537 MB in 120) and where the heads of a group find each
+// other's rows in the L2 (the forty over 8 KV heads: 63.8 us); rows in order at 6.7.  A workgroup
+// alone gets through a row of K and V in 7 ns, which decides where there are few lists.  So:
 //   - A workgroup of four waves walks one list or piece of one (or of four heads, see kSide).  Each wave has a span of 32-row
 //     tiles of its own and LDS that no other wave touches, so the walk needs no workgroup barrier.
 //   - A tile's rows are fetched one tile ahead at head_dim 128, two at 64, into registers.  (Two ahead at 128: 24.6 us against
@@ -542,7 +546,8 @@ static int64_t pieces_per_head(const Shape& s, int64_t units) {
 // Lists whole or in pieces: the less of two sums, in us, from these measurements.
 //   A workgroup alone on its unit takes 7.0 ns per row (head_dim 64: 4.6, whole lists in order 6.0; with half of V 0.78 of that,
 //   with a quarter 0.72), two on one unit 0.7 of their sum; where there are more than two, every one takes 4.5 us beside its
-//   rows. The card reads gathered rows at 4.9 TB/s, rows in order at 5.0, at 6.2 with heads side by side, at 4.2 where every list
+//   rows. The card reads gathered rows at 4.9 TB/s (the rates at the top of the file are lower: they count what a call needs beside
+//   its rows), rows in order at 5.0, at 6.2 with heads side by side, at 4.2 where every list
 //   is a workgroup's own (3.5 where two share V's columns; 64-byte rows two thirds of all that; it includes starting and
 //   draining). Without lists every column tile reads the rows again, from the caches, in pieces at 6.6 TB/s. Pieces cost a second
 //   launch and its latencies (3.3), what is written and read again (2.75 TB/s, without lists 3.5), and for the further sequences

@@ -1335,7 +1335,9 @@ static bool fused_pays(const Shape& s, int es, int32_t pool_w) {
     // Codes stream faster, so that the ranking, which one launch does for one list per compute unit at a time, weighs more:
     // several rounds only for long lists of four heads (27 sequences of 315, 32 heads, window 5, 33.3 us in one launch, 18.4 in
     // two; 28 of 4791, 16 heads x 64, 60.6 / 57.9), and four heads, scored on the matrix cores, in one round down to half full
-    // (32 of 2000 to 8000, 53.5 / 62.1).
+    // (32 of 2000 to 8000, 53.5 / 62.1).  Over 1000 batches the choice is as fast as the better one in the mean, 40 % slower at most:
+    // 26 sequences of 583 to 1189, 32 heads over 8, window 5, 29.3 us in one launch, which ranks sixteen tiles per wave as soon as a
+    // list is longer than 1024, 21.1 in two.
     if (rounds > 1 && (s.group < 4 || s.max_kv <= kFusedWaves * kFusedTilesShort * 64)) return false;
     if (rounds == 1 && s.group == 4 && pool_w == 1) even = 2 * int64_t(s.total_kv) >= int64_t(s.batch) * s.max_kv;
   }
