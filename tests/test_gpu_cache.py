@@ -303,6 +303,18 @@ def test_rows_read_back_are_code_times_scale(dtype, d, hkv, block, layout):
         assert (wide[x][:, 0] == 7).all() and (wide[x][:, -1] == 7).all()
 
 
+@pytest.mark.parametrize("d,block", [(64, 32), (64, 64), (128, 16), (128, 64)])
+def test_fp32_rows_read_back_in_every_shape(d, block):
+    lens = [2 * block + 5, 0, 1, block]
+    c = filled(lens, 3, d, block, 15)
+    c.write(normal(9, 3, d, torch.float32, 17) * 40, normal(9, 3, d, torch.float32, 18), [block - 4, 0, 0, 0], [8, 0, 0, 1])
+    k, v = (torch.full((c.total, 3, d), 7.0, device=DEV) for _ in "kv")
+    say(f"read fp32 d={d} block={block}")
+    hcsa.dllm_hcsa_cache_read(hcsa.make_rows_batch(k, v, c.cu_t, c.total, max(lens)), c.desc, k, v)
+    torch.cuda.synchronize()
+    assert np.array_equal(k.double().cpu().numpy(), c.values("k")) and np.array_equal(v.double().cpu().numpy(), c.values("v"))
+
+
 # ---------------------------------------------------------------- selection
 def read_back(c):
     k, v = (torch.empty((c.total, c.hkv, c.d), dtype=torch.bfloat16, device=DEV) for _ in "kv")
@@ -375,6 +387,26 @@ def test_select_with_two_heads_per_workgroup_and_without(hq, hkv, d, lens):
 def test_select_batches_that_take_one_launch_or_stream_k_once(hq, hkv, batch, n):
     c = filled([n - 13 * b for b in range(batch)], hkv, 128, 32, 51)
     check_select(c, hq, [32] * batch, [m // 5 for m in c.lens], 52)
+
+
+@pytest.mark.parametrize("hq,hkv,d,lens", [
+    (5, 5, 64, [1, 64, 700, 1024]),        # two tiles per wave, one head
+    (8, 2, 64, [1025, 8192, 64, 3000]),    # sixteen, four heads
+    (16, 4, 128, [1024, 8192])])
+def test_select_in_one_launch_at_both_lengths(hq, hkv, d, lens):
+    check_select(filled(lens, hkv, d, 32, 55), hq, [32] * len(lens), [(n + 2) // 3 for n in lens], 56)
+    check_select(filled(lens, hkv, d, 64, 57), hq, [5] * len(lens), [(n + 3) // 4 for n in lens], 58, pool_w=5)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 128), (9, 9, 128), (12, 6, 128), (16, 4, 128), (16, 16, 64), (17, 17, 64), (16, 8, 64), (18, 9, 64), (32, 8, 64)])
+def test_select_over_more_than_64_mib_of_codes(hq, hkv, d):
+    """(From there on rows are read without a place in the caches; every number of heads per pass, with and without pairs of KV heads.)"""
+    n = (64 << 20) // (hkv * d)
+    lens = [n // 13 + 37 * b for b in range(-6, 8)]
+    assert sum(lens) * hkv * d > 64 << 20
+    say(f"select hq={hq} hkv={hkv} d={d}: {sum(lens)} positions")
+    c = filled(lens, hkv, d, 32, 59)
+    check_select(c, hq, [2] * len(lens), [m // 9 for m in lens], 60)
 
 
 # ---------------------------------------------------------------- attention
