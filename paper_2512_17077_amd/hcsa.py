@@ -215,8 +215,9 @@ def _workspace(nbytes: int, device, stream=None) -> Optional[torch.Tensor]:
         return None
     if stream is None:
         return torch.empty(nbytes, dtype=torch.uint8, device=device)   # torch allocations are >= 256-byte aligned
-    if not isinstance(stream, torch.cuda.Stream):   # (anything with a raw stream will do)
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
+    if not isinstance(stream, torch.cuda.Stream):   # (anything with a raw stream will do; 0 is the default one)
+        raw = stream.cuda_stream
+        stream = torch.cuda.ExternalStream(raw, device) if raw else torch.cuda.default_stream(device)
     with torch.cuda.stream(stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 

@@ -82,6 +82,10 @@ def test_a_workspace_is_allocated_on_the_stream_that_uses_it(monkeypatch, librar
     assert took == [side, None] and library.calls[-1][1][-1] == 5
     CALLS[call](x, workspace=torch.zeros(64, dtype=torch.uint8), stream=side)
     assert len(took) == 2   # the caller's own
+    side.cuda_stream = 0   # no handle of an external stream, but the default one
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: "default")
+    CALLS[call](x, stream=side)
+    assert took[2:] == ["default"] and library.calls[-1][1][-1] == 0
 
 
 class Elsewhere(torch.Tensor):

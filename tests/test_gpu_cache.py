@@ -808,6 +808,28 @@ def test_a_call_on_an_idle_stream_takes_no_memory_that_the_current_stream_still_
     assert all(torch.equal(a, b) for a, b in zip(want, got)) and int(got[2].min()) >= 0
 
 
+def test_streams_that_are_not_torchs_own():
+    """An object with a raw stream: another one, and the default stream's 0."""
+    class Raw:
+        device_index = 0
+
+        def __init__(self, raw):
+            self.cuda_stream = raw
+
+    c = filled([9000, 4000], 2, 64, 32, 179)
+    q = normal(2, 4, 64, torch.bfloat16, 180)
+    cu_q, cu_k = (torch.tensor(cu32(x), device=DEV) for x in ([1, 1], [9000, 4000]))
+    batch = hcsa.make_cached_batch(q, cu_q, c.cu_t, c.total, 2, 1, 9000, 0.125)
+    want = run_attend(c, q, cu32([1, 1]), None, cu32([9000, 4000]), 0.125)
+    other = torch.cuda.Stream()
+    for raw in (other.cuda_stream, 0):
+        o = torch.full_like(q, 7.0)
+        torch.cuda.synchronize()
+        hcsa.dllm_hcsa_attend_cached(batch, c.desc, None, cu_k, 13000, 9000, o, stream=Raw(raw))
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)
+
+
 @pytest.mark.parametrize("decode", [False, True])
 def test_a_step_replayed_from_a_hip_graph(decode):
     """Two graphs that share their workspaces, replayed in turn with new rows, queries and places, beside eager work; every
